@@ -612,6 +612,134 @@ int ds_ckpt_restore_parts(const ds_ckpt_reader *const *readers, uint32_t n_parts
                           const ds_plan *plan, uint32_t threads, uint32_t flags, void *compute_stream,
                           ds_event **out);
 
+/* ---- the training step between two snapshots -------------------------------
+ *
+ * Operators of the forward and backward pass that runs while a snapshot drains:
+ * checkpoints of activations in 8 bits, which leave HBM to the staging that
+ * opens the gate early, and the layer norms, products and activations that
+ * write and read them.  They only read the weights, so they may run before the
+ * gate of the snapshot in flight (ds_event_wait_on_stream).
+ *
+ *   - All are asynchronous on `stream`, allocate nothing, keep nothing between
+ *     calls and may be captured into a graph.  A workspace is device memory of
+ *     the caller, 16-byte aligned, of the size that the function's _workspace
+ *     partner names for the same sizes; it may be used by the next call on the
+ *     same stream at once, and its contents mean nothing afterwards.
+ *   - Results do not depend on timing: the same call on the same inputs gives
+ *     the same bytes.
+ *   - Sums, statistics and products are accumulated in 32 bits; a result is
+ *     rounded once, when it is stored (to nearest, ties to even).
+ *   - Memory that a call writes must not overlap what it reads or writes
+ *     otherwise, save where a parameter says so; this is not checked.
+ *   - Nothing is written, and DS_OK returned, where the output has no elements.
+ */
+
+#define DS_MX8 16u /* ds_matrix only: a checkpoint in 8 bits (below); not a type of shards */
+
+/*
+ * A matrix in device memory.  Element (i, j) is at base + itemsize *
+ * (i * row_stride + j * col_stride).  Extents >= 0; the strides of extents > 1
+ * are positive, one of the two is 1 and the other at least the extent of that
+ * one's axis (the strides of extents of 0 and 1 are free).  Where a function
+ * asks for ROWS, col_stride is the one that is 1.  dtype: DS_F32, DS_BF16,
+ * DS_F16, or DS_MX8.
+ *
+ * DS_MX8, always ROWS: 32 neighbouring columns of a row (from column 0 on; the
+ * last group may be short) share a power of two.  scale[i * scale_stride + j / 32]
+ * is the byte E + 127, E = floor(log2(largest magnitude of the group)), at
+ * least -126; base holds int8 codes, each the value divided by 2^(E - 6),
+ * rounded to the nearest whole number (ties to even) and limited to +-127.  The
+ * byte is 0 for a group of zeros, and 255 where any value of it is infinite or
+ * NaN: such a group reads as NaN.  A value is off by at most half a step of
+ * 2^(E - 6), by less than one where it was limited, and is representable in the
+ * type it came from, so that it is read back without another rounding.  Codes
+ * and scales are bytes and can be captured as shards (DS_U8).
+ */
+typedef struct ds_matrix {
+  void *base;
+  uint32_t dtype;
+  uint32_t reserved; /* 0 */
+  int64_t rows, cols;
+  int64_t row_stride, col_stride; /* elements */
+  uint8_t *scale;                 /* DS_MX8, else NULL */
+  int64_t scale_stride;           /* DS_MX8: bytes from row to row, >= ceil(cols / 32); else 0 */
+} ds_matrix;
+
+/* x (DS_F32, DS_BF16, DS_F16; ROWS) into the checkpoint `saved` of the same
+ * extents, and back: x is each value of `saved`, rounded where its type does not
+ * hold it.  Errors: DS_EINVAL, DS_ERANGE, DS_EHIP. */
+int ds_mx8_save(const ds_matrix *x, const ds_matrix *saved, void *stream);
+int ds_mx8_load(const ds_matrix *saved, const ds_matrix *x, void *stream);
+
+/*
+ * Layer norm over the rows of x (DS_F32, DS_BF16, DS_F16; ROWS), eps >= 0:
+ *   mean = sum_j x_j / cols, rstd = 1 / sqrt(sum_j (x_j - mean)^2 / cols + eps),
+ *   y_j = (x_j - mean) * rstd * gamma_j + beta_j.
+ * y: the type and extents of x, ROWS; it may be x itself.  gamma, beta: cols
+ * elements of param_dtype (DS_F32, DS_BF16, DS_F16) in device memory, each may
+ * be NULL (1 and 0).  mean, rstd: one float per row, each may be NULL.  saved:
+ * NULL, or a DS_MX8 matrix of x's extents that x is left in, in the same pass
+ * (x is read before y is written).  A row with a NaN or an infinity gives NaN
+ * in y and rstd, and affects no other row.
+ * Errors: DS_EINVAL, DS_ERANGE, DS_EHIP.
+ */
+int ds_layernorm_forward(const ds_matrix *x, const void *gamma, const void *beta, uint32_t param_dtype, float eps,
+                         const ds_matrix *y, float *mean, float *rstd, const ds_matrix *saved, void *stream);
+
+/*
+ * Its gradient.  With h = (x - mean) * rstd and g = dy * gamma:
+ *   dx = rstd * (g - sum_j g_j / cols - h * sum_j g_j h_j / cols) + residual,
+ *   dgamma_j = sum over rows of dy * h,  dbeta_j = sum over rows of dy.
+ * dy, dx: DS_F32, DS_BF16 or DS_F16, the same for both; ROWS.  x: that type, or the DS_MX8
+ * checkpoint that the forward pass left, whose values then stand for x
+ * everywhere above (mean and rstd are the forward pass's).  residual: NULL, or
+ * the gradient that reaches x past the norm, of dy's type; dx may be residual
+ * or dy itself.  dgamma, dbeta: cols floats, overwritten (with zeros where there
+ * are no rows), each may be NULL.  Errors: DS_EINVAL, DS_ERANGE, DS_EHIP.
+ */
+int ds_layernorm_backward_workspace(int64_t rows, int64_t cols, uint64_t *bytes);
+int ds_layernorm_backward(const ds_matrix *dy, const ds_matrix *x, const float *mean, const float *rstd,
+                          const void *gamma, uint32_t param_dtype, const ds_matrix *residual, const ds_matrix *dx,
+                          float *dgamma, float *dbeta, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* activations */
+#define DS_ACT_NONE 0u
+#define DS_ACT_GELU 1u      /* z * (1 + erf(z / sqrt(2))) / 2                                     */
+#define DS_ACT_GELU_TANH 2u /* z * (1 + tanh(sqrt(2 / pi) * (z + 0.044715 z^3))) / 2              */
+#define DS_ACT_SILU 3u      /* z / (1 + exp(-z))                                                  */
+
+typedef struct ds_matmul_epilogue {
+  const void *bias;          /* NULL, or b.cols elements of bias_dtype in device memory          */
+  uint32_t bias_dtype;       /* DS_F32, DS_BF16 or DS_F16                                        */
+  uint32_t act;              /* DS_ACT_*                                                         */
+  const ds_matrix *residual; /* NULL, or a matrix of c's type and extents, ROWS; may be c itself */
+  const ds_matrix *saved;    /* NULL, or a DS_MX8 matrix of c's extents: z is left in it         */
+} ds_matmul_epilogue;
+
+/*
+ * z = a b + bias,  c = act(z) + residual;  a [m, k], b [k, n], c [m, n].
+ * a and b: DS_BF16 or DS_F16, the same for both, each in either order (a weight
+ * [out, in] is b with row_stride 1).  Either may be DS_MX8 instead: its values
+ * are then rounded to the other's type (to DS_BF16 if both are DS_MX8), which is
+ * exact for a checkpoint of that type.  c: DS_F32, DS_BF16 or DS_F16, ROWS.  epilogue: NULL = all of it absent.
+ * With k = 0 the product is zero.  Errors: DS_EINVAL, DS_ERANGE (an extent
+ * beyond 2^31 - 1 or a workspace too small), DS_EHIP.
+ */
+int ds_matmul_workspace(const ds_matrix *a, const ds_matrix *b, const ds_matrix *c, uint64_t *bytes);
+int ds_matmul(const ds_matrix *a, const ds_matrix *b, const ds_matrix *c, const ds_matmul_epilogue *epilogue,
+              void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * The gradient of c = act(z) with z = product + bias:
+ *   dz = dy * act'(z),  dbias_j = sum over rows of dz (before dz is rounded).
+ * dy, dz: DS_F32, DS_BF16 or DS_F16, the same for both, ROWS; dz may be dy itself.  z: that
+ * type, or a DS_MX8 checkpoint.  dbias: NULL, or cols floats, overwritten (with
+ * zeros where there are no rows).  Errors: DS_EINVAL, DS_ERANGE, DS_EHIP.
+ */
+int ds_activation_backward_workspace(int64_t rows, int64_t cols, uint64_t *bytes);
+int ds_activation_backward(const ds_matrix *dy, const ds_matrix *z, uint32_t act, const ds_matrix *dz, float *dbias,
+                           void *workspace, uint64_t workspace_bytes, void *stream);
+
 /* ---- misc ---------------------------------------------------------------- */
 
 const char *ds_strerror(int code);

@@ -22,6 +22,8 @@ DS_EINVAL, DS_EALIGN, DS_EOVERLAP, DS_EGAP, DS_ERANGE, DS_ENOMEM, DS_EHIP, DS_EB
 DS_EFORMAT = -11
 DS_EFAULT = -12
 DS_ETOOBIG = -13
+DS_MX8 = 16  # ds_matrix only
+DS_ACT_NONE, DS_ACT_GELU, DS_ACT_GELU_TANH, DS_ACT_SILU = 0, 1, 2, 3
 DS_PACK_NOALLOC_TABLE_BYTES = 4 << 20
 DS_FILE_DIRECT, DS_FILE_SYNC, DS_FILE_URING = 1, 2, 4
 DS_PLAN_STRICT, DS_PLAN_HOST_ONLY, DS_PLAN_CHECK_MEMORY = 1, 2, 4
@@ -43,6 +45,8 @@ EXPORTS = [
     "ds_plan_create_files", "ds_layout_assign_files", "ds_plan_file", "ds_plan_shard_file", "ds_flush_start_files",
     "ds_restore_from_files", "ds_ckpt_create_part", "ds_ckpt_flush_snapshot_parts", "ds_ckpt_matches_plan_part",
     "ds_ckpt_restore_parts", "ds_ckpt_append_from",
+    "ds_mx8_save", "ds_mx8_load", "ds_layernorm_forward", "ds_layernorm_backward_workspace", "ds_layernorm_backward",
+    "ds_matmul_workspace", "ds_matmul", "ds_activation_backward_workspace", "ds_activation_backward",
 ]
 
 
@@ -122,6 +126,30 @@ class ds_ckpt_tensor(ctypes.Structure):
     ]
 
 
+class ds_matrix(ctypes.Structure):
+    _fields_ = [
+        ("base", ctypes.c_void_p),
+        ("dtype", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32),
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64),
+        ("col_stride", ctypes.c_int64),
+        ("scale", ctypes.c_void_p),
+        ("scale_stride", ctypes.c_int64),
+    ]
+
+
+class ds_matmul_epilogue(ctypes.Structure):
+    _fields_ = [
+        ("bias", ctypes.c_void_p),
+        ("bias_dtype", ctypes.c_uint32),
+        ("act", ctypes.c_uint32),
+        ("residual", ctypes.POINTER(ds_matrix)),
+        ("saved", ctypes.POINTER(ds_matrix)),
+    ]
+
+
 class DsError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -170,6 +198,7 @@ def _load() -> ctypes.CDLL:
     L = ctypes.CDLL(LIB_PATH)
     vp, u64, u32, sz = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_size_t
     P = ctypes.POINTER
+    i64, mat = ctypes.c_int64, P(ds_matrix)
     sig = {
         "ds_itemsize": ([u32], ctypes.c_int),
         "ds_layout_assign": ([P(ds_shard_desc), sz, u64, P(u64)], ctypes.c_int),
@@ -231,6 +260,15 @@ def _load() -> ctypes.CDLL:
         "ds_ckpt_flush_snapshot_parts": ([P(vp), u32, vp, u32], ctypes.c_int),
         "ds_ckpt_matches_plan_part": ([vp, vp, u32], ctypes.c_int),
         "ds_ckpt_restore_parts": ([P(vp), u32, vp, vp, u32, u32, vp, P(vp)], ctypes.c_int),
+        "ds_mx8_save": ([mat, mat, vp], ctypes.c_int),
+        "ds_mx8_load": ([mat, mat, vp], ctypes.c_int),
+        "ds_layernorm_forward": ([mat, vp, vp, u32, ctypes.c_float, mat, vp, vp, mat, vp], ctypes.c_int),
+        "ds_layernorm_backward_workspace": ([i64, i64, P(u64)], ctypes.c_int),
+        "ds_layernorm_backward": ([mat, mat, vp, vp, vp, u32, mat, mat, vp, vp, vp, u64, vp], ctypes.c_int),
+        "ds_matmul_workspace": ([mat, mat, mat, P(u64)], ctypes.c_int),
+        "ds_matmul": ([mat, mat, mat, P(ds_matmul_epilogue), vp, u64, vp], ctypes.c_int),
+        "ds_activation_backward_workspace": ([i64, i64, P(u64)], ctypes.c_int),
+        "ds_activation_backward": ([mat, mat, u32, mat, vp, vp, u64, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -677,3 +715,119 @@ def ds_image_compress(image_dev: int, nbytes: int, block_bytes: int, keep_dev: i
                       packed_dev: int, stream: int = 0) -> None:
     _check(_lib.ds_image_compress(image_dev, nbytes, block_bytes, keep_dev, pos_dev, patterns_dev, packed_dev, stream),
            "ds_image_compress")
+
+
+# ---- the training step between two snapshots ----------------------------------
+
+_float_codes = None
+
+
+def _float_code(dtype) -> int:
+    global _float_codes
+    if _float_codes is None:
+        import torch
+        _float_codes = {torch.float32: DS_F32, torch.bfloat16: DS_BF16, torch.float16: DS_F16}
+    code = _float_codes.get(dtype)
+    if code is None:
+        raise TypeError(f"dtype {dtype} is none of float32, bfloat16 and float16")
+    return code
+
+
+def make_matrix(tensor) -> ds_matrix:
+    """A 2-D torch tensor on the GPU (any strides that ds_matrix takes: slices, transposes) as a ds_matrix.  The caller
+    keeps the tensor alive for as long as the matrix is used."""
+    code = _float_code(tensor.dtype)
+    if not tensor.is_cuda:
+        raise ValueError("the tensor is not in device memory")
+    if tensor.dim() != 2:
+        raise ValueError(f"a matrix has two dimensions, the tensor has {tensor.dim()}")
+    (rows, cols), (down, across) = tensor.shape, tensor.stride()
+    return ds_matrix(tensor.data_ptr(), code, 0, rows, cols, down, across, None, 0)
+
+
+def make_mx8(codes, scale) -> ds_matrix:
+    """A checkpoint in 8 bits out of two torch tensors on the GPU: int8 codes [rows, cols] and uint8 scales
+    [rows, ceil(cols / 32)], both with neighbouring columns next to each other."""
+    import torch
+    if codes.dtype != torch.int8 or scale.dtype != torch.uint8:
+        raise TypeError("codes are int8, scales uint8")
+    if not (codes.is_cuda and scale.is_cuda):
+        raise ValueError("codes and scales are in device memory")
+    if codes.dim() != 2 or scale.dim() != 2:
+        raise ValueError("codes and scales have two dimensions")
+    rows, cols = codes.shape
+    if tuple(scale.shape) != (rows, -(-cols // 32)):
+        raise ValueError(f"codes of {rows} x {cols} have scales of {rows} x {-(-cols // 32)}, not {tuple(scale.shape)}")
+    if scale.shape[1] > 1 and scale.stride(1) != 1:
+        raise ValueError("the scales of a row are not next to each other")
+    return ds_matrix(codes.data_ptr(), DS_MX8, 0, rows, cols, codes.stride(0), codes.stride(1), scale.data_ptr(), scale.stride(0))
+
+
+def make_epilogue(bias=None, act: int = DS_ACT_NONE, residual: Optional[ds_matrix] = None,
+                  saved: Optional[ds_matrix] = None) -> ds_matmul_epilogue:
+    """`bias`: a 1-D torch tensor on the GPU, contiguous.  (The structure keeps the matrices it points to alive, but no
+    tensor's memory.)"""
+    ep = ds_matmul_epilogue(None, DS_F32, act)
+    if bias is not None:
+        ep.bias_dtype = _float_code(bias.dtype)
+        if not bias.is_cuda:
+            raise ValueError("the bias is not in device memory")
+        if bias.dim() != 1 or (bias.shape[0] > 1 and bias.stride(0) != 1):
+            raise ValueError("a bias is one contiguous dimension")
+        ep.bias = bias.data_ptr()
+    if residual is not None:
+        ep.residual = ctypes.pointer(residual)
+    if saved is not None:
+        ep.saved = ctypes.pointer(saved)
+    return ep
+
+
+def _workspace_bytes(rc: int, out, where: str) -> int:
+    _check(rc, where)
+    return out.value
+
+
+def ds_mx8_save(x: ds_matrix, saved: ds_matrix, stream: int = 0) -> None:
+    _check(_lib.ds_mx8_save(x, saved, stream), "ds_mx8_save")
+
+
+def ds_mx8_load(saved: ds_matrix, x: ds_matrix, stream: int = 0) -> None:
+    _check(_lib.ds_mx8_load(saved, x, stream), "ds_mx8_load")
+
+
+def ds_layernorm_forward(x: ds_matrix, gamma: Optional[int], beta: Optional[int], param_dtype: int, eps: float, y: ds_matrix,
+                         mean: Optional[int] = None, rstd: Optional[int] = None, saved: Optional[ds_matrix] = None,
+                         stream: int = 0) -> None:
+    _check(_lib.ds_layernorm_forward(x, gamma, beta, param_dtype, eps, y, mean, rstd, saved, stream), "ds_layernorm_forward")
+
+
+def ds_layernorm_backward_workspace(rows: int, cols: int) -> int:
+    out = ctypes.c_uint64(0)
+    return _workspace_bytes(_lib.ds_layernorm_backward_workspace(rows, cols, out), out, "ds_layernorm_backward_workspace")
+
+
+def ds_layernorm_backward(dy: ds_matrix, x: ds_matrix, mean: int, rstd: int, gamma: Optional[int], param_dtype: int,
+                          residual: Optional[ds_matrix], dx: ds_matrix, dgamma: Optional[int], dbeta: Optional[int],
+                          workspace: Optional[int], workspace_bytes: int, stream: int = 0) -> None:
+    _check(_lib.ds_layernorm_backward(dy, x, mean, rstd, gamma, param_dtype, residual, dx, dgamma, dbeta, workspace,
+                                      workspace_bytes, stream), "ds_layernorm_backward")
+
+
+def ds_matmul_workspace(a: ds_matrix, b: ds_matrix, c: ds_matrix) -> int:
+    out = ctypes.c_uint64(0)
+    return _workspace_bytes(_lib.ds_matmul_workspace(a, b, c, out), out, "ds_matmul_workspace")
+
+
+def ds_matmul(a: ds_matrix, b: ds_matrix, c: ds_matrix, epilogue: Optional[ds_matmul_epilogue] = None,
+              workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(_lib.ds_matmul(a, b, c, epilogue, workspace, workspace_bytes, stream), "ds_matmul")
+
+
+def ds_activation_backward_workspace(rows: int, cols: int) -> int:
+    out = ctypes.c_uint64(0)
+    return _workspace_bytes(_lib.ds_activation_backward_workspace(rows, cols, out), out, "ds_activation_backward_workspace")
+
+
+def ds_activation_backward(dy: ds_matrix, z: ds_matrix, act: int, dz: ds_matrix, dbias: Optional[int],
+                           workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(_lib.ds_activation_backward(dy, z, act, dz, dbias, workspace, workspace_bytes, stream), "ds_activation_backward")

@@ -1,0 +1,170 @@
+// Checkpoints of activations in 8 bits: written, read back, and the backward pass of an activation that reads one.
+//
+// All three are bound by HBM: a few operations for each value that is read or written once.  A lane holds eight
+// neighbouring columns, which is one 16-byte access of a 16-bit type and 8 bytes of codes, and four lanes a group of 32
+// that shares a scale: its largest magnitude is two moves between lanes of a quad, and the scale is one byte that the
+// first of the four writes.  The scale is a power of two, so that x / step is exact before it is rounded to a whole number
+// and the value that is read back has at most 7 significant bits, which every type holds.
+
+#include <type_traits>
+
+#include "ds_ops.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// Work items are pieces of eight columns; a row has a multiple of four of them, so that a group's are four neighbouring lanes.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void ds_mx8_save_kernel(Rows x, Rows saved, int64_t rows, int64_t cols, uint32_t pieces) {
+  for (int64_t first = (int64_t)blockIdx.x * kThreads; first < rows * pieces; first += (int64_t)gridDim.x * kThreads) {
+    const int64_t i = (first + threadIdx.x) / pieces, j = (first + threadIdx.x) % pieces * 8, left = i < rows ? cols - j : 0;
+    const int n = (int)(left < 8 ? left : 8);
+    mx8_put(saved, i, j, n, RowsOf<T>::get(x, i, j, n));
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void ds_mx8_load_kernel(Rows saved, Rows x, int64_t rows, int64_t cols, uint32_t pieces) {
+  for (int64_t first = (int64_t)blockIdx.x * kThreads; first < rows * pieces; first += (int64_t)gridDim.x * kThreads) {
+    const int64_t i = (first + threadIdx.x) / pieces, j = (first + threadIdx.x) % pieces * 8, left = i < rows ? cols - j : 0;
+    const int n = (int)(left < 8 ? left : 8);
+    put_up_to8<T>(x.base, i * x.stride + j, n, RowsOf<Mx8>::get(saved, i, j, n));
+  }
+}
+
+int check_pair(const ds_matrix *x, const ds_matrix *saved) {
+  DS_TRY(ds_check_matrix(x, true));
+  DS_TRY(ds_check_matrix(saved, true));
+  return x->dtype == DS_MX8 || saved->dtype != DS_MX8 || !ds_same_extents(x, saved) ? DS_EINVAL : DS_OK;
+}
+
+template <bool SAVE>
+int launch_mx8(const ds_matrix *x, const ds_matrix *saved, hipStream_t stream) {
+  DS_TRY(check_pair(x, saved));
+  if (x->rows == 0 || x->cols == 0) return DS_OK;
+  const int64_t pieces = ds_groups(x->cols) * (kGroup / 8), all = (x->rows * pieces + kThreads - 1) / kThreads;
+  const int64_t grid = all < kMaxGrid ? all : kMaxGrid;
+  return ds_with_type(x->dtype, [&](auto type) -> int {
+    typedef decltype(type) T;
+    if (SAVE)
+      hipLaunchKernelGGL(ds_mx8_save_kernel<T>, dim3((uint32_t)grid), dim3(kThreads), 0, stream, ds_rows(x), ds_rows(saved), x->rows,
+                         x->cols, (uint32_t)pieces);
+    else
+      hipLaunchKernelGGL(ds_mx8_load_kernel<T>, dim3((uint32_t)grid), dim3(kThreads), 0, stream, ds_rows(saved), ds_rows(x), x->rows,
+                         x->cols, (uint32_t)pieces);
+    DS_HIP_TRY(hipGetLastError());
+    return DS_OK;
+  });
+}
+
+// A work-group takes 64 pieces of eight columns and every (4 * parts)-th row of them for each of its four wavefronts; the
+// sums over its rows are one line of `partial`.
+template <typename T, typename Z, uint32_t ACT>
+__global__ __launch_bounds__(kThreads) void ds_activation_backward_kernel(Rows dy, Rows z, Rows dz, int64_t rows, int64_t cols,
+                                                                          float *partial) {
+  __shared__ float sums[4][64][8 + 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t j = ((int64_t)blockIdx.x * 64 + lane) * 8, left = cols - j;
+  const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
+  Eight sum = {};
+  for (int64_t i = (int64_t)blockIdx.y * 4 + wave; i < rows; i += (int64_t)gridDim.y * 4) {
+    const Eight d = RowsOf<T>::get(dy, i, j, n), at = RowsOf<Z>::get(z, i, j, n);
+    Eight r;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      r.v[k] = d.v[k] * activation_slope<ACT>(at.v[k]);
+      sum.v[k] += r.v[k];
+    }
+    put_up_to8<T>(dz.base, i * dz.stride + j, n, r);
+  }
+  if (!partial) return;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sums[wave][lane][k] = sum.v[k];
+  __syncthreads();
+  for (int c = threadIdx.x; c < 512; c += kThreads) {
+    const int64_t col = (int64_t)blockIdx.x * 512 + c;
+    if (col < cols)
+      partial[blockIdx.y * cols + col] = sums[0][c / 8][c % 8] + sums[1][c / 8][c % 8] + sums[2][c / 8][c % 8] + sums[3][c / 8][c % 8];
+  }
+}
+
+// partial[p][j] summed over p: a work-group has 64 columns, each of its four wavefronts a quarter of the parts.
+__global__ __launch_bounds__(kThreads) void ds_sum_parts_kernel(const float *partial, int64_t parts, int64_t cols, float *out) {
+  __shared__ float sums[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t j = (int64_t)blockIdx.x * 64 + lane;
+  const int64_t each = (parts + 3) / 4, first = wave * each, last = first + each < parts ? first + each : parts;
+  float sum = 0.f;
+  if (j < cols)
+    for (int64_t p = first; p < last; ++p) sum += partial[p * cols + j];
+  sums[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && j < cols) out[j] = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
+}
+
+constexpr int64_t kActGroups = 2048;  // work-groups of a launch, about
+int64_t act_parts(int64_t rows, int64_t cols) {
+  const int64_t across = cols > 512 ? (cols + 511) / 512 : 1, by_rows = (rows + 3) / 4, by_grid = (kActGroups + across - 1) / across;
+  const int64_t parts = by_rows < by_grid ? by_rows : by_grid;
+  return parts < 1 ? 1 : parts > 65535 ? 65535 : parts;
+}
+
+}  // namespace
+
+int ds_launch_sum_parts(const float *partial, int64_t parts, int64_t cols, float *out, hipStream_t stream) {
+  hipLaunchKernelGGL(ds_sum_parts_kernel, dim3((uint32_t)((cols + 63) / 64)), dim3(kThreads), 0, stream, partial, parts, cols, out);
+  DS_HIP_TRY(hipGetLastError());
+  return DS_OK;
+}
+
+extern "C" int ds_mx8_save(const ds_matrix *x, const ds_matrix *saved, void *stream) {
+  return launch_mx8<true>(x, saved, (hipStream_t)stream);
+}
+
+extern "C" int ds_mx8_load(const ds_matrix *saved, const ds_matrix *x, void *stream) {
+  return launch_mx8<false>(x, saved, (hipStream_t)stream);
+}
+
+extern "C" int ds_activation_backward_workspace(int64_t rows, int64_t cols, uint64_t *bytes) {
+  if (!bytes || rows < 0 || cols < 0) return DS_EINVAL;
+  if (rows > kMaxExtent || cols > kMaxExtent) return DS_ERANGE;
+  *bytes = (uint64_t)(act_parts(rows, cols) * cols * 4);
+  return DS_OK;
+}
+
+extern "C" int ds_activation_backward(const ds_matrix *dy, const ds_matrix *z, uint32_t act, const ds_matrix *dz, float *dbias,
+                                      void *workspace, uint64_t workspace_bytes, void *stream) {
+  DS_TRY(ds_check_matrix(dy, true));
+  DS_TRY(ds_check_matrix(z, true));
+  DS_TRY(ds_check_matrix(dz, true));
+  if (dy->dtype == DS_MX8 || dz->dtype != dy->dtype || (z->dtype != DS_MX8 && z->dtype != dy->dtype) || act > DS_ACT_SILU ||
+      !ds_same_extents(dy, z) || !ds_same_extents(dy, dz) || ds_misaligned(dbias, 4))
+    return DS_EINVAL;
+  const int64_t rows = dy->rows, cols = dy->cols, parts = act_parts(rows, cols);
+  if (cols == 0 || (rows == 0 && !dbias)) return DS_OK;
+  if (dbias) {
+    if (!workspace || ds_misaligned(workspace, 16)) return DS_EINVAL;
+    if (workspace_bytes < (uint64_t)(parts * cols * 4)) return DS_ERANGE;
+  }
+  hipStream_t st = (hipStream_t)stream;
+  if (rows > 0) {
+    const dim3 grid((uint32_t)((cols + 511) / 512), (uint32_t)parts);
+    const int rc = ds_with_type(dy->dtype, [&](auto type) -> int {
+      typedef decltype(type) T;
+      return ds_with_act(act, [&](auto a) -> int {
+        constexpr uint32_t A = decltype(a)::value;
+        if (z->dtype == DS_MX8)
+          hipLaunchKernelGGL((ds_activation_backward_kernel<T, Mx8, A>), grid, dim3(kThreads), 0, st, ds_rows(dy), ds_rows(z),
+                             ds_rows(dz), rows, cols, dbias ? (float *)workspace : nullptr);
+        else
+          hipLaunchKernelGGL((ds_activation_backward_kernel<T, T, A>), grid, dim3(kThreads), 0, st, ds_rows(dy), ds_rows(z),
+                             ds_rows(dz), rows, cols, dbias ? (float *)workspace : nullptr);
+        DS_HIP_TRY(hipGetLastError());
+        return DS_OK;
+      });
+    });
+    DS_TRY(rc);
+  }
+  return dbias ? ds_launch_sum_parts((const float *)workspace, rows > 0 ? parts : 0, cols, dbias, st) : DS_OK;
+}
