@@ -134,7 +134,7 @@ __device__ inline void put_in_lds(uint16_t *lds, bool k_last, u32x4 x) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void ds_matmul_kernel(Operand a, Operand b, Epilogue e, int64_t depth) {
+__global__ __launch_bounds__(kThreads) void ds_matmul_kernel(Operand a, Operand b, Epilogue e, int64_t depth, uint32_t across) {
   __shared__ union {
     struct {
       alignas(16) uint16_t a[kTile * kPitch], b[kTile * kPitch];
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kThreads) void ds_matmul_kernel(Operand a, Operand 
     float out[kTile][kTile + 4];
   } lds;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t p0 = (int64_t)blockIdx.y * kTile, q0 = (int64_t)blockIdx.x * kTile;
+  const int64_t p0 = (int64_t)(blockIdx.x / across) * kTile, q0 = (int64_t)(blockIdx.x % across) * kTile;
   int pa, ka, pb, kb;
   place(a.k_last, pa, ka);
   place(b.k_last, pb, kb);
@@ -175,6 +175,206 @@ __global__ __launch_bounds__(kThreads) void ds_matmul_kernel(Operand a, Operand 
   }
 }
 
+// ---- tiles whose operands go to LDS directly ---------------------------------------------------------------------
+
+constexpr int kStep = 64;  // of k: what one stage of LDS holds
+
+// An operand as these kernels have it: 16-byte aligned, every line a whole number of 16-byte pieces apart and long.
+struct Source {
+  const uint8_t *base;
+  int64_t ld;      // bytes
+  int64_t extent;  // of p
+};
+
+struct TileArgs {
+  Source a, b;
+  int64_t depth;
+  uint32_t tiles_m, tiles_n, splits;
+  float *partial;  // [splits][m][n], or NULL: the epilogue follows at once
+};
+
+// Lane l of a wavefront brings 16 bytes from resource + offset to LDS at m0 + 16 l.  An offset of kNowhere reads zeros.
+// Written by hand because the compiler would otherwise wait for the transfers of the next stage before it reads this one.
+constexpr uint32_t kNowhere = 0x80000000u;
+__device__ inline void to_lds(uint32_t lds, uint32_t offset, u32x4 resource) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(resource) : "memory");
+}
+__device__ inline void stage_is_there() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The part of one operand that a work-group stages: P lines or columns, kStep of k.
+//   K_LAST: LDS holds P rows of 128 bytes, eight pieces of eight k; piece c of row r is at c ^ (r % 8), so that the 16 rows of
+//     an operand's read, all at one c, lie in different banks.
+//   else: LDS holds kStep rows of P elements.  A lane's eight k are then in eight rows: ds_read_b64_tr_b16 reads four rows of 16
+//     elements with 16 lanes and gives each lane one column of them.  Pairs of pieces are exchanged by the row, so that
+//     the 32 lanes of a pass, eight rows of 32 bytes, meet every bank once.
+template <int P, int WAVES, bool K_LAST>
+struct Stage {
+  static constexpr int kBytes = P * kStep * 2, kLoads = kBytes / 1024 / WAVES, kLine = P * 2;
+  static_assert(kBytes % (1024 * WAVES) == 0, "whole transfers for each wavefront");
+  uint32_t offset[kLoads];  // of this lane's pieces from the operand's first element of the stage
+  int at_k[kLoads];         // their place along k
+  static __device__ inline int turn(int k) {
+    return P % 128 == 0 ? (k & 3) | (k >> 3 & 1) << 2 : (k >> 1 & 1) | (k >> 3 & 1) << 1;
+  }
+
+  __device__ inline void begin(const Source &s, int64_t p0, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int f = (wave * kLoads + i) * 64 + lane;
+      if (K_LAST) {
+        const int r = f / 8, c = (f % 8) ^ (r & 7);
+        at_k[i] = c * 8;
+        offset[i] = p0 + r < s.extent ? (uint32_t)(r * s.ld + c * 16) : kNowhere;
+      } else {
+        const int r = f / (P / 8), c = (f % (P / 8)) ^ (2 * turn(r));
+        at_k[i] = r;
+        offset[i] = p0 + c * 8 < s.extent ? (uint32_t)(r * s.ld + c * 16) : kNowhere;
+      }
+    }
+  }
+  // Starts the transfers of step `step` into LDS at `lds`; `left`: what of k there is from the step's first on.
+  __device__ inline void bring(const Source &s, int64_t p0, int64_t step, int64_t left, uint32_t lds, int wave) const {
+    const uint64_t from = (uint64_t)s.base + (K_LAST ? p0 * s.ld + step * (kStep * 2) : step * kStep * s.ld + p0 * 2);
+    u32x4 resource;
+    resource[0] = __builtin_amdgcn_readfirstlane((uint32_t)from), resource[1] = __builtin_amdgcn_readfirstlane((uint32_t)(from >> 32));
+    resource[2] = kNowhere, resource[3] = 0x00020000;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      uint32_t o = offset[i];
+      if (left < kStep) o = at_k[i] < left ? o : kNowhere;
+      to_lds(lds + (wave * kLoads + i) * 1024, o, resource);
+    }
+  }
+  // The operand of a matrix instruction: 16 lines from p (a multiple of 16) on, k from 32 * half on.
+  static __device__ inline u32x4 read(const uint8_t *lds, int p, int half, int lane) {
+    if (K_LAST) {
+      const int r = p + lane % 16, c = (half * 4 + lane / 16) ^ (lane & 7);
+      return *(const u32x4 *)(lds + r * 128 + c * 16);
+    }
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 *Place;
+    const int k = half * 32 + lane / 16 * 8 + lane % 16 / 4;
+    const uint8_t *at = lds + k * kLine + (((p / 16) ^ turn(k)) * 32) + lane % 4 * 8;
+    const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)at), high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + 4 * kLine));
+    return __builtin_bit_cast(u32x4, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// Tiles of (WM * MI * 16) x (WN * 64), a wavefront has MI * 16 rows of 64 columns.  Two stages of LDS: while the matrix
+// instructions run on one, the transfers of the next step fill the other; one barrier a step.
+template <typename T, int MI, int WM, int WN, bool A_K, bool B_K>
+__global__ __launch_bounds__(WM *WN * 64) void ds_matmul_tile_kernel(TileArgs t, Epilogue e) {
+  constexpr int kWaves = WM * WN, kM = WM * MI * 16, kN = WN * 64;
+  typedef Stage<kM, kWaves, A_K> A;
+  typedef Stage<kN, kWaves, B_K> B;
+  constexpr int kStage = A::kBytes + B::kBytes, kOutPitch = 68;
+  static_assert(kWaves * 16 * kOutPitch * 4 <= 2 * kStage, "the sums leave through the stages");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  // Work-groups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, in stripes of four tiles' rows, so that
+  // what its work-groups read at a time stays in its L2.
+  const uint32_t tiles = t.tiles_m * t.tiles_n, all = tiles * t.splits, each = all / 8, more = all % 8;
+  const uint32_t xcd = blockIdx.x % 8, id = xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8;
+  const uint32_t split = id / tiles, tile = id % tiles, stripe = tile / (4 * t.tiles_n), in_stripe = tile % (4 * t.tiles_n);
+  const uint32_t high = t.tiles_m - stripe * 4 < 4 ? t.tiles_m - stripe * 4 : 4;
+  const int64_t p0 = (int64_t)(stripe * 4 + in_stripe % high) * kM, q0 = (int64_t)(in_stripe / high) * kN;
+
+  const int64_t steps = (t.depth + kStep - 1) / kStep, first = steps * split / t.splits, last = steps * (split + 1) / t.splits;
+  A a;
+  B b;
+  a.begin(t.a, p0, wave, lane);
+  b.begin(t.b, q0, wave, lane);
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+  const auto bring = [&](int64_t step, int which) {
+    a.bring(t.a, p0, step, t.depth - step * kStep, base + which * kStage, wave);
+    b.bring(t.b, q0, step, t.depth - step * kStep, base + which * kStage + A::kBytes, wave);
+  };
+  const int m0 = wave / WN * MI * 16, n0 = wave % WN * 64;
+  f32x4 sum[MI][4] = {};
+  bring(first, 0);
+  for (int64_t step = first; step < last; ++step) {
+    const int which = (int)(step - first) & 1;
+    stage_is_there();
+    if (step + 1 < last) bring(step + 1, which ^ 1);
+    const uint8_t *in_a = lds + which * kStage, *in_b = in_a + A::kBytes;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      u32x4 y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = B::read(in_b, n0 + j * 16, half, lane);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const u32x4 x = A::read(in_a, m0 + i * 16, half, lane);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[i][j] = mfma(y[j], x, sum[i][j], T());
+      }
+    }
+  }
+  // a lane's sums: row lane % 16 of the 16, columns 16 j + 4 (lane / 16) and on
+  if (t.partial) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int64_t row = p0 + m0 + i * 16 + lane % 16;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t col = q0 + n0 + j * 16 + lane / 16 * 4;
+        float *to = t.partial + ((int64_t)split * e.m + row) * e.n + col;
+        if (row < e.m)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (col + k < e.n) to[k] = sum[i][j][k];
+      }
+    }
+    return;
+  }
+  __syncthreads();
+  float *out = (float *)lds + wave * 16 * kOutPitch;
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *(f32x4 *)(out + lane % 16 * kOutPitch + j * 16 + lane / 16 * 4) = sum[i][j];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int row = r * 8 + lane / 8, col = lane % 8 * 8;
+      Eight z;
+      const f32x4 lo = *(const f32x4 *)(out + row * kOutPitch + col), hi = *(const f32x4 *)(out + row * kOutPitch + col + 4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) z.v[k] = lo[k], z.v[4 + k] = hi[k];
+      const int64_t at = p0 + m0 + i * 16 + row, j = q0 + n0 + col, left = at < e.m ? e.n - j : 0;
+      finish8(e, at, j, (int)(left < 0 ? 0 : left < 8 ? left : 8), z);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The sums of the splits, in their order, and the epilogue.  A row has a multiple of four pieces of eight columns.
+__global__ __launch_bounds__(kThreads) void ds_matmul_join_kernel(const float *partial, uint32_t splits, uint32_t pieces, Epilogue e) {
+  for (int64_t first = (int64_t)blockIdx.x * kThreads; first < e.m * pieces; first += (int64_t)gridDim.x * kThreads) {
+    const int64_t i = (first + threadIdx.x) / pieces, j = (first + threadIdx.x) % pieces * 8, left = i < e.m ? e.n - j : 0;
+    const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
+    Eight z = {};
+    for (uint32_t s = 0; s < splits; ++s) {
+      const Eight p = get_up_to8<float>(partial, (s * e.m + i) * e.n + j, n);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) z.v[k] += p.v[k];
+    }
+    finish8(e, i, j, n, z);
+  }
+}
+
+// An operand's lines of `length` elements as lines of 16-bit values, a multiple of eight of them, the rest zeros.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void ds_matmul_lines_kernel(Operand o, int64_t lines, int64_t length, uint16_t *out, uint32_t pieces) {
+  for (int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x; at < lines * pieces; at += (int64_t)gridDim.x * kThreads) {
+    const int64_t line = at / pieces, j = at % pieces * 8;
+    *(u32x4 *)(out + at * 8) = o.k_last ? bring8<T>(o, line, j, length) : bring8<T>(o, j, line, lines);
+  }
+}
+
 // a (or b's transpose): p along `along` = its rows if `p_rows`.
 Operand operand(const ds_matrix *m, bool p_rows) {
   const int64_t p = p_rows ? m->rows : m->cols, k = p_rows ? m->cols : m->rows;
@@ -197,12 +397,115 @@ int check_product(const ds_matrix *a, const ds_matrix *b, const ds_matrix *c) {
   return DS_OK;
 }
 
+
+// ---- how a product is computed ---------------------------------------------------------------------------------------
+
+enum class Way { kSimple, kTile };
+struct Choice {
+  Way way;
+  int tile;         // index into kTiles
+  uint32_t splits;
+  bool lines_a, lines_b;  // is the operand laid out in the workspace first?
+  uint64_t at_a, at_b, at_partial, bytes;
+};
+struct TileSize {
+  int m, n, at_once;  // at_once: work-groups on a CU
+};
+constexpr TileSize kTiles[] = {{256, 256, 1}, {192, 256, 1}, {128, 256, 1}, {128, 128, 2}, {64, 64, 4}};
+
+// May the operand be read in 16-byte pieces, all within its lines?
+bool in_pieces(const Operand &o, int64_t depth) {
+  const int64_t length = o.k_last ? depth : o.extent;
+  return !o.scale && !ds_misaligned(o.base, 16) && length % 8 == 0 && (o.ld % 8 == 0) && o.ld < (1 << 21);
+}
+uint64_t lines_bytes(const Operand &o, int64_t depth) {
+  const int64_t lines = o.k_last ? o.extent : depth, length = o.k_last ? depth : o.extent;
+  return (uint64_t)(lines * ((length + 7) / 8 * 8) * 2 + 127) / 128 * 128;
+}
+
+Choice choose(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t depth) {
+  Choice c{Way::kSimple, 0, 1, false, false, 0, 0, 0, 0};
+  if (depth == 0 || m * n * depth < (1 << 18)) return c;
+  // lines of 16-bit values are at most 2^22 bytes apart, so that a stage's offsets have 31 bits
+  const auto too_long = [&](const Operand &o) { return (o.k_last ? depth : o.extent) > (1 << 21); };
+  if (too_long(a) || too_long(b)) return c;
+  c.way = Way::kTile;
+  c.lines_a = !in_pieces(a, depth), c.lines_b = !in_pieces(b, depth);
+  double best = 1e300;
+  const int64_t steps = (depth + kStep - 1) / kStep;
+  for (int i = 0; i < 5; ++i) {
+    const TileSize &s = kTiles[i];
+    const int64_t tiles = ((m + s.m - 1) / s.m) * ((n + s.n - 1) / s.n), room = 256 * s.at_once;
+    for (int64_t splits = 1; splits <= 16 && splits * 4 <= steps + 3; ++splits) {
+      const int64_t rounds = (tiles * splits + room - 1) / room;
+      double cost = (double)rounds * s.m * s.n * s.at_once * ((steps + splits - 1) / splits + 4);
+      if (splits > 1) cost += (double)m * n * splits * 0.5;
+      if (cost < best) best = cost, c.tile = i, c.splits = (uint32_t)splits;
+    }
+  }
+  if (c.lines_a) c.at_a = c.bytes, c.bytes += lines_bytes(a, depth);
+  if (c.lines_b) c.at_b = c.bytes, c.bytes += lines_bytes(b, depth);
+  if (c.splits > 1) c.at_partial = c.bytes, c.bytes += (uint64_t)c.splits * m * n * 4;
+  return c;
+}
+
+template <typename T>
+int launch_lines(const Operand &o, int64_t depth, uint8_t *out, Source *s, hipStream_t stream) {
+  const int64_t lines = o.k_last ? o.extent : depth, length = o.k_last ? depth : o.extent, pieces = (length + 7) / 8;
+  const int64_t groups = (lines * pieces + kThreads - 1) / kThreads;
+  hipLaunchKernelGGL(ds_matmul_lines_kernel<T>, dim3((uint32_t)(groups < kMaxGrid ? groups : kMaxGrid)), dim3(kThreads), 0, stream, o, lines,
+                     length, (uint16_t *)out, (uint32_t)pieces);
+  DS_HIP_TRY(hipGetLastError());
+  // (the zeros behind a line of p are columns of no output)
+  *s = Source{out, pieces * 16, o.k_last ? o.extent : pieces * 8};
+  return DS_OK;
+}
+
+template <typename T, int MI, int WM, int WN>
+int launch_tile(const Operand &a, const Operand &b, const TileArgs &t, const Epilogue &e, hipStream_t stream) {
+  const dim3 grid(t.tiles_m * t.tiles_n * t.splits), threads(WM * WN * 64);
+  if (a.k_last && b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, WM, WN, true, true>), grid, threads, 0, stream, t, e);
+  else if (a.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, WM, WN, true, false>), grid, threads, 0, stream, t, e);
+  else if (b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, WM, WN, false, true>), grid, threads, 0, stream, t, e);
+  else hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, WM, WN, false, false>), grid, threads, 0, stream, t, e);
+  DS_HIP_TRY(hipGetLastError());
+  return DS_OK;
+}
+
+template <typename T>
+int launch_product(const Operand &a, const Operand &b, const Epilogue &e, int64_t depth, const Choice &c, uint8_t *ws, hipStream_t stream) {
+  if (c.way == Way::kSimple) {
+    const int64_t across = (e.n + kTile - 1) / kTile, down = (e.m + kTile - 1) / kTile;
+    hipLaunchKernelGGL(ds_matmul_kernel<T>, dim3((uint32_t)(across * down)), dim3(kThreads), 0, stream, a, b, e, depth, (uint32_t)across);
+    DS_HIP_TRY(hipGetLastError());
+    return DS_OK;
+  }
+  const TileSize &s = kTiles[c.tile];
+  TileArgs t{{(const uint8_t *)a.base, a.ld * 2, a.extent}, {(const uint8_t *)b.base, b.ld * 2, b.extent}, depth,
+             (uint32_t)((e.m + s.m - 1) / s.m), (uint32_t)((e.n + s.n - 1) / s.n), c.splits, c.splits > 1 ? (float *)(ws + c.at_partial) : nullptr};
+  if (c.lines_a) DS_TRY(launch_lines<T>(a, depth, ws + c.at_a, &t.a, stream));
+  if (c.lines_b) DS_TRY(launch_lines<T>(b, depth, ws + c.at_b, &t.b, stream));
+  switch (c.tile) {
+    case 0: DS_TRY((launch_tile<T, 8, 2, 4>(a, b, t, e, stream))); break;
+    case 1: DS_TRY((launch_tile<T, 6, 2, 4>(a, b, t, e, stream))); break;
+    case 2: DS_TRY((launch_tile<T, 4, 2, 4>(a, b, t, e, stream))); break;
+    case 3: DS_TRY((launch_tile<T, 4, 2, 2>(a, b, t, e, stream))); break;
+    default: DS_TRY((launch_tile<T, 1, 4, 1>(a, b, t, e, stream))); break;
+  }
+  if (c.splits == 1) return DS_OK;
+  const int64_t pieces = ds_groups(e.n) * (kGroup / 8), groups = (e.m * pieces + kThreads - 1) / kThreads;
+  hipLaunchKernelGGL(ds_matmul_join_kernel, dim3((uint32_t)(groups < kMaxGrid ? groups : kMaxGrid)), dim3(kThreads), 0, stream, t.partial,
+                     t.splits, (uint32_t)pieces, e);
+  DS_HIP_TRY(hipGetLastError());
+  return DS_OK;
+}
+
 }  // namespace
 
 extern "C" int ds_matmul_workspace(const ds_matrix *a, const ds_matrix *b, const ds_matrix *c, uint64_t *bytes) {
   if (!bytes) return DS_EINVAL;
   DS_TRY(check_product(a, b, c));
-  *bytes = 0;
+  *bytes = choose(operand(a, true), operand(b, false), c->rows, c->cols, a->cols).bytes;
   return DS_OK;
 }
 
@@ -221,16 +524,16 @@ extern "C" int ds_matmul(const ds_matrix *a, const ds_matrix *b, const ds_matrix
     if (ep.saved->dtype != DS_MX8 || !ds_same_extents(ep.saved, c)) return DS_EINVAL;
   }
   if (c->rows == 0 || c->cols == 0) return DS_OK;
-  (void)workspace, (void)workspace_bytes;
   const Operand oa = operand(a, true), ob = operand(b, false);
+  const Choice how = choose(oa, ob, c->rows, c->cols, a->cols);
+  if (how.bytes) {
+    if (!workspace || ds_misaligned(workspace, 16)) return DS_EINVAL;
+    if (workspace_bytes < how.bytes) return DS_ERANGE;
+  }
   const Epilogue e{ds_rows(c), ds_rows(ep.residual), ds_rows(ep.saved), ep.bias, c->rows, c->cols, c->dtype, ep.bias_dtype, ep.act};
-  const dim3 grid((uint32_t)((c->cols + kTile - 1) / kTile), (uint32_t)((c->rows + kTile - 1) / kTile));
-  if (grid.y > 65535) return DS_ERANGE;
-  hipStream_t st = (hipStream_t)stream;
+  // work-groups of a launch: of 64 x 64, the smallest tile
+  if (((c->rows + 63) / 64) * ((c->cols + 63) / 64) > kMaxGrid) return DS_ERANGE;
   if (a->dtype == DS_F16 || b->dtype == DS_F16)
-    hipLaunchKernelGGL(ds_matmul_kernel<__half>, grid, dim3(kThreads), 0, st, oa, ob, e, a->cols);
-  else
-    hipLaunchKernelGGL(ds_matmul_kernel<__hip_bfloat16>, grid, dim3(kThreads), 0, st, oa, ob, e, a->cols);
-  DS_HIP_TRY(hipGetLastError());
-  return DS_OK;
+    return launch_product<__half>(oa, ob, e, a->cols, how, (uint8_t *)workspace, (hipStream_t)stream);
+  return launch_product<__hip_bfloat16>(oa, ob, e, a->cols, how, (uint8_t *)workspace, (hipStream_t)stream);
 }
