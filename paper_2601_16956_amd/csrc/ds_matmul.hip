@@ -177,7 +177,7 @@ __global__ __launch_bounds__(kThreads) void ds_matmul_kernel(Operand a, Operand 
 
 // ---- tiles whose operands go to LDS directly ---------------------------------------------------------------------
 
-constexpr int kStep = 64;  // of k: what one stage of LDS holds
+constexpr int kStep = 32;  // of k: what one stage of LDS holds, and one matrix instruction takes
 
 // An operand as these kernels have it: 16-byte aligned, every line a whole number of 16-byte pieces apart and long.
 struct Source {
@@ -199,20 +199,29 @@ constexpr uint32_t kNowhere = 0x80000000u;
 __device__ inline void to_lds(uint32_t lds, uint32_t offset, u32x4 resource) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(resource) : "memory");
 }
-__device__ inline void stage_is_there() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All but the last LATER transfers of this wavefront are done, and what it has read of LDS is in registers; then the same
+// holds for the work-group.
+template <int LATER>
+__device__ inline void stage_is_there() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
+}
 
 // The part of one operand that a work-group stages: P lines or columns, kStep of k.
-//   K_LAST: LDS holds P rows of 128 bytes, eight pieces of eight k; piece c of row r is at c ^ (r % 8), so that the 16 rows of
-//     an operand's read, all at one c, lie in different banks.
+//   K_LAST: LDS holds P rows of 64 bytes, four pieces of eight k; piece c of row r is at c ^ turn_row(r).  A read takes 16 lanes
+//     at a time, lanes 0-3, 12-15 and 20-27 first: rows 0-3 and 12-15 at one c and rows 4-11 at the next, which then lie in
+//     different banks.
 //   else: LDS holds kStep rows of P elements.  A lane's eight k are then in eight rows: ds_read_b64_tr_b16 reads four rows of 16
 //     elements with 16 lanes and gives each lane one column of them.  Pairs of pieces are exchanged by the row, so that
 //     the 32 lanes of a pass, eight rows of 32 bytes, meet every bank once.
 template <int P, int WAVES, bool K_LAST>
 struct Stage {
-  static constexpr int kBytes = P * kStep * 2, kLoads = kBytes / 1024 / WAVES, kLine = P * 2;
-  static_assert(kBytes % (1024 * WAVES) == 0, "whole transfers for each wavefront");
+  static constexpr int kBytes = P * kStep * 2, kTransfers = kBytes / 1024, kLoads = (kTransfers + WAVES - 1) / WAVES, kLine = P * 2;
+  // Every wavefront starts kLoads transfers, so that all count alike; those that are too many bring zeros to LDS that nobody reads.
+  static constexpr int kSpare = kLoads * WAVES > kTransfers ? 1024 : 0;
+  static_assert(kBytes % 1024 == 0, "whole transfers");
   uint32_t offset[kLoads];  // of this lane's pieces from the operand's first element of the stage
   int at_k[kLoads];         // their place along k
+  static __device__ inline int turn_row(int r) { return (r >> 2 & 3) ^ (r >> 1 & 2); }
   static __device__ inline int turn(int k) {
     return P % 128 == 0 ? (k & 3) | (k >> 3 & 1) << 2 : (k >> 1 & 1) | (k >> 3 & 1) << 1;
   }
@@ -220,9 +229,11 @@ struct Stage {
   __device__ inline void begin(const Source &s, int64_t p0, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int f = (wave * kLoads + i) * 64 + lane;
+      const int f = (i * WAVES + wave) * 64 + lane;
+      at_k[i] = 0, offset[i] = kNowhere;
+      if (i * WAVES + wave >= kTransfers) continue;
       if (K_LAST) {
-        const int r = f / 8, c = (f % 8) ^ (r & 7);
+        const int r = f / 4, c = (f % 4) ^ turn_row(r);
         at_k[i] = c * 8;
         offset[i] = p0 + r < s.extent ? (uint32_t)(r * s.ld + c * 16) : kNowhere;
       } else {
@@ -232,44 +243,40 @@ struct Stage {
       }
     }
   }
-  // Starts the transfers of step `step` into LDS at `lds`; `left`: what of k there is from the step's first on.
-  __device__ inline void bring(const Source &s, int64_t p0, int64_t step, int64_t left, uint32_t lds, int wave) const {
-    const uint64_t from = (uint64_t)s.base + (K_LAST ? p0 * s.ld + step * (kStep * 2) : step * kStep * s.ld + p0 * 2);
-    u32x4 resource;
-    resource[0] = __builtin_amdgcn_readfirstlane((uint32_t)from), resource[1] = __builtin_amdgcn_readfirstlane((uint32_t)(from >> 32));
-    resource[2] = kNowhere, resource[3] = 0x00020000;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      uint32_t o = offset[i];
-      if (left < kStep) o = at_k[i] < left ? o : kNowhere;
-      to_lds(lds + (wave * kLoads + i) * 1024, o, resource);
-    }
+  // Where the first step's transfers read from, and how far apart the steps are.
+  static __device__ inline uint64_t place(const Source &s, int64_t p0, int64_t step) {
+    return (uint64_t)s.base + (K_LAST ? p0 * s.ld + step * (kStep * 2) : step * kStep * s.ld + p0 * 2);
   }
-  // The operand of a matrix instruction: 16 lines from p (a multiple of 16) on, k from 32 * half on.
-  static __device__ inline u32x4 read(const uint8_t *lds, int p, int half, int lane) {
-    if (K_LAST) {
-      const int r = p + lane % 16, c = (half * 4 + lane / 16) ^ (lane & 7);
-      return *(const u32x4 *)(lds + r * 128 + c * 16);
-    }
+  static __device__ inline int64_t apart(const Source &s) { return K_LAST ? kStep * 2 : kStep * s.ld; }
+  // Starts this wavefront's transfer `i` of the step at `from` into the stage at `lds`; `left`: what of k there is from the
+  // step's first on, 0 and less where nothing is.
+  __device__ inline void bring(int i, uint64_t from, int left, uint32_t lds, uint32_t spare, int wave) const {
+    const int x = i * WAVES + wave;
+    const u32x4 resource = {(uint32_t)from, (uint32_t)(from >> 32), kNowhere, 0x00020000u};
+    to_lds(kSpare == 0 || x < kTransfers ? lds + x * 1024 : spare, at_k[i] < left ? offset[i] : kNowhere, resource);
+  }
+  // The operand of a matrix instruction: 16 lines from p (a multiple of 16) on.
+  static __device__ inline u32x4 read(const uint8_t *lds, int p, int lane) {
+    if (K_LAST) return *(const u32x4 *)(lds + (p + lane % 16) * 64 + ((lane / 16) ^ turn_row(lane)) * 16);
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4 *Place;
-    const int k = half * 32 + lane / 16 * 8 + lane % 16 / 4;
+    const int k = lane / 16 * 8 + lane % 16 / 4;
     const uint8_t *at = lds + k * kLine + (((p / 16) ^ turn(k)) * 32) + lane % 4 * 8;
     const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)at), high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + 4 * kLine));
     return __builtin_bit_cast(u32x4, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
 
-// Tiles of (WM * MI * 16) x (WN * 64), a wavefront has MI * 16 rows of 64 columns.  Two stages of LDS: while the matrix
-// instructions run on one, the transfers of the next step fill the other; one barrier a step.
-template <typename T, int MI, int WM, int WN, bool A_K, bool B_K>
-__global__ __launch_bounds__(WM *WN * 64) void ds_matmul_tile_kernel(TileArgs t, Epilogue e) {
-  constexpr int kWaves = WM * WN, kM = WM * MI * 16, kN = WN * 64;
+// Tiles of (WM * MI * 16) x (WN * NI * 16), a wavefront has MI * 16 rows of NI * 16 columns.  STAGES stages of LDS: while the matrix
+// instructions run on one, the transfers of the others are under way; one barrier a step.
+template <typename T, int MI, int NI, int WM, int WN, int STAGES, bool A_K, bool B_K>
+__global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs t, Epilogue e) {
+  constexpr int kWaves = WM * WN, kM = WM * MI * 16, kN = WN * NI * 16;
   typedef Stage<kM, kWaves, A_K> A;
   typedef Stage<kN, kWaves, B_K> B;
-  constexpr int kStage = A::kBytes + B::kBytes, kOutPitch = 68;
-  static_assert(kWaves * 16 * kOutPitch * 4 <= 2 * kStage, "the sums leave through the stages");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
+  constexpr int kStage = A::kBytes + B::kBytes, kOutPitch = NI * 16 + 4;
+  static_assert(kWaves * 16 * kOutPitch * 4 <= STAGES * kStage, "the sums leave through the stages");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES * kStage + (A::kSpare | B::kSpare)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // Work-groups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, in stripes of four tiles' rows, so that
@@ -286,38 +293,70 @@ __global__ __launch_bounds__(WM *WN * 64) void ds_matmul_tile_kernel(TileArgs t,
   a.begin(t.a, p0, wave, lane);
   b.begin(t.b, q0, wave, lane);
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-  const auto bring = [&](int64_t step, int which) {
-    a.bring(t.a, p0, step, t.depth - step * kStep, base + which * kStage, wave);
-    b.bring(t.b, q0, step, t.depth - step * kStep, base + which * kStage + A::kBytes, wave);
+  // The step whose transfers start next.
+  uint64_t from_a = A::place(t.a, p0, first), from_b = B::place(t.b, q0, first);
+  const int64_t apart_a = A::apart(t.a), apart_b = B::apart(t.b);
+  int left = (int)((last * kStep < t.depth ? last * kStep : t.depth) - first * kStep);
+  constexpr int kLoads = A::kLoads + B::kLoads;
+  const auto bring = [&](int i, int to) {
+    if (i < A::kLoads) a.bring(i, from_a, left, base + to * kStage, base + STAGES * kStage, wave);
+    else b.bring(i - A::kLoads, from_b, left, base + to * kStage + A::kBytes, base + STAGES * kStage, wave);
+    if (i == kLoads - 1) from_a += apart_a, from_b += apart_b, left -= kStep;
   };
-  const int m0 = wave / WN * MI * 16, n0 = wave % WN * 64;
-  f32x4 sum[MI][4] = {};
-  bring(first, 0);
-  for (int64_t step = first; step < last; ++step) {
-    const int which = (int)(step - first) & 1;
-    stage_is_there();
-    if (step + 1 < last) bring(step + 1, which ^ 1);
-    const uint8_t *in_a = lds + which * kStage, *in_b = in_a + A::kBytes;
+  const int m0 = wave / WN * MI * 16, n0 = wave % WN * NI * 16;
+  f32x4 sum[MI][NI] = {};
+  struct Operands {
+    u32x4 x[MI], y[NI];
+  } even, odd;
+  const auto fetch = [&](Operands &o, const uint8_t *stage, int i) {
+    if (i < NI) o.y[i] = B::read(stage + A::kBytes, n0 + i * 16, lane);
+    else o.x[i - NI] = A::read(stage, m0 + (i - NI) * 16, lane);
+  };
+  // One step on the operands in `now`, while the next step's come from the stage `next_at` and a later step's go to the stage
+  // `to`.  Reads and transfers stand between the matrix instructions: a wavefront that starts all its transfers at once waits
+  // for the unit that takes them, 16 cycles for each.  (Transfers behind the last step bring zeros.)
+  const auto advance = [&](const Operands &now, Operands &next, int next_at, int to) {
+    const uint8_t *stage = lds + next_at * kStage;
+    int read = 0, brought = 0;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      u32x4 y[4];
+    for (int i = 0; i < MI; ++i) {
+      // (MI + NI) reads and kLoads transfers in as many parts as there are rows
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = B::read(in_b, n0 + j * 16, half, lane);
+      for (; read < (MI + NI) * (i + 1) / MI; ++read) fetch(next, stage, read);
 #pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        const u32x4 x = A::read(in_a, m0 + i * 16, half, lane);
+      for (; brought < kLoads * (i + 1) / MI; ++brought) bring(brought, to);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[i][j] = mfma(y[j], x, sum[i][j], T());
-      }
+      for (int j = 0; j < NI; ++j) sum[i][j] = mfma(now.y[j], now.x[i], sum[i][j], T());
+      __builtin_amdgcn_sched_barrier(0);
     }
+  };
+  const auto after = [](int stage) { return stage + 1 == STAGES ? 0 : stage + 1; };
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s)
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) bring(i, s);
+  stage_is_there<(STAGES - 2) * kLoads>();
+#pragma unroll
+  for (int i = 0; i < MI + NI; ++i) fetch(even, lds, i);
+  // Two steps, s and s + 1, for a barrier: before them the operands of s are in registers, and the stages of s + 1 and s + 2 have to
+  // be there; those of s and before are free, for the transfers of s + STAGES - 1 and s + STAGES.  An odd last step's
+  // partner is zeros.
+  int at = 0;
+  for (int64_t step = first; step < last; step += 2) {
+    stage_is_there<(STAGES - 4) * kLoads>();
+    const int one = after(at), two = after(one);
+    advance(even, odd, one, at == 0 ? STAGES - 1 : at - 1);
+    advance(odd, even, two, at);
+    at = two;
   }
+  stage_is_there<0>();
   // a lane's sums: row lane % 16 of the 16, columns 16 j + 4 (lane / 16) and on
   if (t.partial) {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const int64_t row = p0 + m0 + i * 16 + lane % 16;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < NI; ++j) {
         const int64_t col = q0 + n0 + j * 16 + lane / 16 * 4;
         float *to = t.partial + ((int64_t)split * e.m + row) * e.n + col;
         if (row < e.m)
@@ -328,17 +367,16 @@ __global__ __launch_bounds__(WM *WN * 64) void ds_matmul_tile_kernel(TileArgs t,
     }
     return;
   }
-  __syncthreads();
   float *out = (float *)lds + wave * 16 * kOutPitch;
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) *(f32x4 *)(out + lane % 16 * kOutPitch + j * 16 + lane / 16 * 4) = sum[i][j];
+    for (int j = 0; j < NI; ++j) *(f32x4 *)(out + lane % 16 * kOutPitch + j * 16 + lane / 16 * 4) = sum[i][j];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const int row = r * 8 + lane / 8, col = lane % 8 * 8;
+#pragma unroll 1
+    for (int r = 0; r < NI / 2; ++r) {
+      const int row = (r * 64 + lane) / (NI * 2), col = lane % (NI * 2) * 8;
       Eight z;
       const f32x4 lo = *(const f32x4 *)(out + row * kOutPitch + col), hi = *(const f32x4 *)(out + row * kOutPitch + col + 4);
 #pragma unroll
@@ -436,10 +474,10 @@ Choice choose(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t 
   for (int i = 0; i < 5; ++i) {
     const TileSize &s = kTiles[i];
     const int64_t tiles = ((m + s.m - 1) / s.m) * ((n + s.n - 1) / s.n), room = 256 * s.at_once;
-    for (int64_t splits = 1; splits <= 16 && splits * 4 <= steps + 3; ++splits) {
+    for (int64_t splits = 1; splits <= 16 && splits * 8 <= steps + 7; ++splits) {
       const int64_t rounds = (tiles * splits + room - 1) / room;
-      double cost = (double)rounds * s.m * s.n * s.at_once * ((steps + splits - 1) / splits + 4);
-      if (splits > 1) cost += (double)m * n * splits * 0.5;
+      double cost = (double)rounds * s.m * s.n * s.at_once * ((steps + splits - 1) / splits + 8);
+      if (splits > 1) cost += (double)m * n * splits * 1.0;
       if (cost < best) best = cost, c.tile = i, c.splits = (uint32_t)splits;
     }
   }
@@ -461,13 +499,13 @@ int launch_lines(const Operand &o, int64_t depth, uint8_t *out, Source *s, hipSt
   return DS_OK;
 }
 
-template <typename T, int MI, int WM, int WN>
+template <typename T, int MI, int NI, int WM, int WN, int STAGES>
 int launch_tile(const Operand &a, const Operand &b, const TileArgs &t, const Epilogue &e, hipStream_t stream) {
   const dim3 grid(t.tiles_m * t.tiles_n * t.splits), threads(WM * WN * 64);
-  if (a.k_last && b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, WM, WN, true, true>), grid, threads, 0, stream, t, e);
-  else if (a.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, WM, WN, true, false>), grid, threads, 0, stream, t, e);
-  else if (b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, WM, WN, false, true>), grid, threads, 0, stream, t, e);
-  else hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, WM, WN, false, false>), grid, threads, 0, stream, t, e);
+  if (a.k_last && b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, true, true>), grid, threads, 0, stream, t, e);
+  else if (a.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, true, false>), grid, threads, 0, stream, t, e);
+  else if (b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, false, true>), grid, threads, 0, stream, t, e);
+  else hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, false, false>), grid, threads, 0, stream, t, e);
   DS_HIP_TRY(hipGetLastError());
   return DS_OK;
 }
@@ -486,11 +524,11 @@ int launch_product(const Operand &a, const Operand &b, const Epilogue &e, int64_
   if (c.lines_a) DS_TRY(launch_lines<T>(a, depth, ws + c.at_a, &t.a, stream));
   if (c.lines_b) DS_TRY(launch_lines<T>(b, depth, ws + c.at_b, &t.b, stream));
   switch (c.tile) {
-    case 0: DS_TRY((launch_tile<T, 8, 2, 4>(a, b, t, e, stream))); break;
-    case 1: DS_TRY((launch_tile<T, 6, 2, 4>(a, b, t, e, stream))); break;
-    case 2: DS_TRY((launch_tile<T, 4, 2, 4>(a, b, t, e, stream))); break;
-    case 3: DS_TRY((launch_tile<T, 4, 2, 2>(a, b, t, e, stream))); break;
-    default: DS_TRY((launch_tile<T, 1, 4, 1>(a, b, t, e, stream))); break;
+    case 0: DS_TRY((launch_tile<T, 8, 4, 2, 4, 5>(a, b, t, e, stream))); break;
+    case 1: DS_TRY((launch_tile<T, 6, 4, 2, 4, 5>(a, b, t, e, stream))); break;
+    case 2: DS_TRY((launch_tile<T, 4, 4, 2, 4, 6>(a, b, t, e, stream))); break;
+    case 3: DS_TRY((launch_tile<T, 4, 4, 2, 2, 5>(a, b, t, e, stream))); break;
+    default: DS_TRY((launch_tile<T, 1, 4, 4, 1, 5>(a, b, t, e, stream))); break;
   }
   if (c.splits == 1) return DS_OK;
   const int64_t pieces = ds_groups(e.n) * (kGroup / 8), groups = (e.m * pieces + kThreads - 1) / kThreads;
