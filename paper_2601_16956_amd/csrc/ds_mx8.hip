@@ -15,20 +15,23 @@ namespace {
 constexpr int kThreads = 256;
 
 // Work items are pieces of eight columns; a row has a multiple of four of them, so that a group's are four neighbouring lanes.
-template <typename T>
+// (A division in 64 bits takes as long as the rest.  Index: uint32_t where it holds their number.)
+template <typename T, typename Index>
 __global__ __launch_bounds__(kThreads) void ds_mx8_save_kernel(Rows x, Rows saved, int64_t rows, int64_t cols, uint32_t pieces) {
   for (int64_t first = (int64_t)blockIdx.x * kThreads; first < rows * pieces; first += (int64_t)gridDim.x * kThreads) {
-    const int64_t i = (first + threadIdx.x) / pieces, j = (first + threadIdx.x) % pieces * 8, left = i < rows ? cols - j : 0;
-    const int n = (int)(left < 8 ? left : 8);
+    const Index item = (Index)(first + threadIdx.x), row = item / (Index)pieces;
+    const int64_t i = row, j = (int64_t)(item - row * (Index)pieces) * 8, left = i < rows ? cols - j : 0;
+    const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
     mx8_put(saved, i, j, n, RowsOf<T>::get(x, i, j, n));
   }
 }
 
-template <typename T>
+template <typename T, typename Index>
 __global__ __launch_bounds__(kThreads) void ds_mx8_load_kernel(Rows saved, Rows x, int64_t rows, int64_t cols, uint32_t pieces) {
   for (int64_t first = (int64_t)blockIdx.x * kThreads; first < rows * pieces; first += (int64_t)gridDim.x * kThreads) {
-    const int64_t i = (first + threadIdx.x) / pieces, j = (first + threadIdx.x) % pieces * 8, left = i < rows ? cols - j : 0;
-    const int n = (int)(left < 8 ? left : 8);
+    const Index item = (Index)(first + threadIdx.x), row = item / (Index)pieces;
+    const int64_t i = row, j = (int64_t)(item - row * (Index)pieces) * 8, left = i < rows ? cols - j : 0;
+    const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
     put_up_to8<T>(x.base, i * x.stride + j, n, RowsOf<Mx8>::get(saved, i, j, n));
   }
 }
@@ -45,36 +48,41 @@ int launch_mx8(const ds_matrix *x, const ds_matrix *saved, hipStream_t stream) {
   if (x->rows == 0 || x->cols == 0) return DS_OK;
   const int64_t pieces = ds_groups(x->cols) * (kGroup / 8), all = (x->rows * pieces + kThreads - 1) / kThreads;
   const int64_t grid = all < kMaxGrid ? all : kMaxGrid;
+  const bool narrow = all <= (int64_t)0xffffffff / kThreads;
   return ds_with_type(x->dtype, [&](auto type) -> int {
     typedef decltype(type) T;
-    if (SAVE)
-      hipLaunchKernelGGL(ds_mx8_save_kernel<T>, dim3((uint32_t)grid), dim3(kThreads), 0, stream, ds_rows(x), ds_rows(saved), x->rows,
-                         x->cols, (uint32_t)pieces);
-    else
-      hipLaunchKernelGGL(ds_mx8_load_kernel<T>, dim3((uint32_t)grid), dim3(kThreads), 0, stream, ds_rows(saved), ds_rows(x), x->rows,
-                         x->cols, (uint32_t)pieces);
-    DS_HIP_TRY(hipGetLastError());
-    return DS_OK;
+    const auto launch = [&](auto kernel, const ds_matrix *from, const ds_matrix *to) -> int {
+      hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(kThreads), 0, stream, ds_rows(from), ds_rows(to), x->rows, x->cols, (uint32_t)pieces);
+      DS_HIP_TRY(hipGetLastError());
+      return DS_OK;
+    };
+    if (SAVE) return narrow ? launch(ds_mx8_save_kernel<T, uint32_t>, x, saved) : launch(ds_mx8_save_kernel<T, uint64_t>, x, saved);
+    return narrow ? launch(ds_mx8_load_kernel<T, uint32_t>, saved, x) : launch(ds_mx8_load_kernel<T, uint64_t>, saved, x);
   });
 }
 
-// A work-group takes 64 pieces of eight columns and every (4 * parts)-th row of them for each of its four wavefronts; the
-// sums over its rows are one line of `partial`.
+// A work-group takes 64 pieces of eight columns and every (4 * parts)-th row of them for each of its four wavefronts, which ask for the
+// next row before they compute on this one; the sums over its rows are one line of `partial`.
 template <typename T, typename Z, uint32_t ACT>
 __global__ __launch_bounds__(kThreads) void ds_activation_backward_kernel(Rows dy, Rows z, Rows dz, int64_t rows, int64_t cols,
                                                                           float *partial) {
   __shared__ float sums[4][64][8 + 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t j = ((int64_t)blockIdx.x * 64 + lane) * 8, left = cols - j;
+  const int64_t j = ((int64_t)blockIdx.x * 64 + lane) * 8, left = cols - j, stride = (int64_t)gridDim.y * 4;
   const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
   Eight sum = {};
-  for (int64_t i = (int64_t)blockIdx.y * 4 + wave; i < rows; i += (int64_t)gridDim.y * 4) {
-    const Eight d = RowsOf<T>::get(dy, i, j, n), at = RowsOf<Z>::get(z, i, j, n);
+  int64_t i = (int64_t)blockIdx.y * 4 + wave;
+  auto next_d = RowsOf<T>::ask(dy, i, j, i < rows ? n : 0);
+  auto next_at = RowsOf<Z>::ask(z, i, j, i < rows ? n : 0);
+  for (; i < rows; i += stride) {
+    const Eight d = RowsOf<T>::value(next_d, n), at = RowsOf<Z>::value(next_at, n);
+    const int more = i + stride < rows ? n : 0;
+    next_d = RowsOf<T>::ask(dy, i + stride, j, more), next_at = RowsOf<Z>::ask(z, i + stride, j, more);
     Eight r;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       r.v[k] = d.v[k] * activation_slope<ACT>(at.v[k]);
-      sum.v[k] += r.v[k];
+      sum.v[k] += k < n ? r.v[k] : 0.f;
     }
     put_up_to8<T>(dz.base, i * dz.stride + j, n, r);
   }
@@ -89,18 +97,31 @@ __global__ __launch_bounds__(kThreads) void ds_activation_backward_kernel(Rows d
   }
 }
 
-// partial[p][j] summed over p: a work-group has 64 columns, each of its four wavefronts a quarter of the parts.
-__global__ __launch_bounds__(kThreads) void ds_sum_parts_kernel(const float *partial, int64_t parts, int64_t cols, float *out) {
-  __shared__ float sums[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t j = (int64_t)blockIdx.x * 64 + lane;
-  const int64_t each = (parts + 3) / 4, first = wave * each, last = first + each < parts ? first + each : parts;
-  float sum = 0.f;
-  if (j < cols)
-    for (int64_t p = first; p < last; ++p) sum += partial[p * cols + j];
-  sums[wave][lane] = sum;
+// The lines of `partial` added: a work-group has 16 columns, and each of its 16 rows of threads every 16th line; then those 16 sums
+// in their order.  blockIdx.y: the first or the second set of lines.
+__global__ __launch_bounds__(kThreads) void ds_sum_parts_kernel(const float *partial, int64_t parts, int64_t cols, float *out0, float *out1) {
+  __shared__ float sums[16][16 + 1];
+  const int across = threadIdx.x % 16, row = threadIdx.x / 16;
+  const int64_t j = (int64_t)blockIdx.x * 16 + across;
+  float *out = blockIdx.y ? out1 : out0;
+  const float *from = partial + blockIdx.y * parts * cols + j;
+  if (!out) return;
+  float sum[4] = {};
+  if (j < cols) {
+    int64_t p = row;
+    for (; p + 48 < parts; p += 64)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) sum[u] += from[(p + 16 * u) * cols];
+    for (; p < parts; p += 16) sum[0] += from[p * cols];
+  }
+  sums[row][across] = sum[0] + sum[1] + (sum[2] + sum[3]);
   __syncthreads();
-  if (wave == 0 && j < cols) out[j] = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
+  if (row == 0 && j < cols) {
+    float s = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s += sums[r][across];
+    out[j] = s;
+  }
 }
 
 constexpr int64_t kActGroups = 2048;  // work-groups of a launch, about
@@ -112,8 +133,9 @@ int64_t act_parts(int64_t rows, int64_t cols) {
 
 }  // namespace
 
-int ds_launch_sum_parts(const float *partial, int64_t parts, int64_t cols, float *out, hipStream_t stream) {
-  hipLaunchKernelGGL(ds_sum_parts_kernel, dim3((uint32_t)((cols + 63) / 64)), dim3(kThreads), 0, stream, partial, parts, cols, out);
+int ds_launch_sum_parts(const float *partial, int64_t parts, int64_t cols, float *out0, float *out1, hipStream_t stream) {
+  hipLaunchKernelGGL(ds_sum_parts_kernel, dim3((uint32_t)((cols + 15) / 16), out1 ? 2 : 1), dim3(kThreads), 0, stream, partial, parts, cols,
+                     out0, out1);
   DS_HIP_TRY(hipGetLastError());
   return DS_OK;
 }
@@ -166,5 +188,5 @@ extern "C" int ds_activation_backward(const ds_matrix *dy, const ds_matrix *z, u
     });
     DS_TRY(rc);
   }
-  return dbias ? ds_launch_sum_parts((const float *)workspace, rows > 0 ? parts : 0, cols, dbias, st) : DS_OK;
+  return dbias ? ds_launch_sum_parts((const float *)workspace, rows > 0 ? parts : 0, cols, dbias, nullptr, st) : DS_OK;
 }

@@ -244,33 +244,59 @@ inline Rows ds_rows(const ds_matrix *m) {
 // Marks the type of a checkpoint in 8 bits where a template takes an element type.
 struct Mx8 {};
 
-// The first n <= 8 of eight values from column j (a multiple of 8) of row i on; the others are 0.
+// The first n <= 8 of eight values from column j (a multiple of 8) of row i on; the others are 0.  In two halves, so that a kernel can
+// ask for a row long before it computes on it: ask() loads the bits, value() makes floats of them.
 template <typename T>
 struct RowsOf {
-  static __device__ inline Eight get(const Rows &m, int64_t i, int64_t j, int n) {
-    return get_up_to8<T>(m.base, i * m.stride + j, n);
+  struct Bits {
+    ds_u32x4 w[sizeof(T) / 2];
+  };
+  static __device__ inline Bits ask(const Rows &m, int64_t i, int64_t j, int n) {
+    Bits b = {};
+    const T *from = (const T *)m.base + i * m.stride + j;
+    if (n >= 8) {
+#pragma unroll
+      for (int k = 0; k < (int)sizeof(T) / 2; ++k) b.w[k] = ((const ds_u32x4 *)from)[k];
+    } else if (sizeof(T) == 4) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < n) b.w[k / 4][k % 4] = ((const uint32_t *)from)[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < n) b.w[0][k / 2] |= (uint32_t)((const uint16_t *)from)[k] << (16 * (k % 2));
+    }
+    return b;
   }
+  static __device__ inline Eight value(const Bits &b, int) { return Elem<T>::get8(&b, 0); }
+  static __device__ inline Eight get(const Rows &m, int64_t i, int64_t j, int n) { return value(ask(m, i, j, n), n); }
 };
 template <>
 struct RowsOf<Mx8> {
-  static __device__ inline Eight get(const Rows &m, int64_t i, int64_t j, int n) {
+  struct Bits {
+    ds_u32x2 codes;
+    uint32_t scale;
+  };
+  static __device__ inline Bits ask(const Rows &m, int64_t i, int64_t j, int n) {
+    Bits b = {};
     const uint8_t *codes = (const uint8_t *)m.base + i * m.stride + j;
-    ds_u32x2 q;
-    q[0] = q[1] = 0;
-    float step = 0.f;
-    if (n > 0) step = mx8_step(m.scale[i * m.scale_stride + j / kGroup]);
-    if (n >= 8) q = *(const ds_u32x2 *)codes;
+    if (n > 0) b.scale = m.scale[i * m.scale_stride + j / kGroup];
+    if (n >= 8) b.codes = *(const ds_u32x2 *)codes;
     else
 #pragma unroll
       for (int k = 0; k < 8; ++k)
-        if (k < n) q[k / 4] |= (uint32_t)codes[k] << (8 * (k % 4));
-    Eight e = mx8_values(q, step);
+        if (k < n) b.codes[k / 4] |= (uint32_t)codes[k] << (8 * (k % 4));
+    return b;
+  }
+  static __device__ inline Eight value(const Bits &b, int n) {
+    Eight e = mx8_values(b.codes, mx8_step(b.scale));
     if (n < 8) {  // a step of NaN is not to reach the places beyond the row
 #pragma unroll
       for (int k = 0; k < 8; ++k) e.v[k] = k < n ? e.v[k] : 0.f;
     }
     return e;
   }
+  static __device__ inline Eight get(const Rows &m, int64_t i, int64_t j, int n) { return value(ask(m, i, j, n), n); }
 };
 
 // Leaves eight values (n <= 8 of them in the row, the others 0) of row i from column j on in a checkpoint.  All lanes of
@@ -291,7 +317,8 @@ __device__ inline void mx8_put(const Rows &m, int64_t i, int64_t j, int n, const
 // ---- device: activations ---------------------------------------------------------------------------------------
 
 // 1 / (1 + exp(-x)): exp overflows to infinity for very negative x, and the quotient is then 0, its limit.
-__device__ inline float sigmoid(float x) { return 1.f / (1.f + __expf(-x)); }
+// v_rcp_f32 is off by one unit of the last place at most, a division in full takes ten instructions more.
+__device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
 constexpr float kGeluTanh = 0.7978845608028654f;  // sqrt(2 / pi)
 constexpr float kGeluCube = 0.044715f;
 
@@ -338,5 +365,6 @@ __device__ inline float wave_sum(float x) {
   return x;
 }
 
-// out[j] = partial[0][j] + partial[1][j] + ... over `parts` lines of `cols`, in an order that only their number decides.
-int ds_launch_sum_parts(const float *partial, int64_t parts, int64_t cols, float *out, hipStream_t stream);
+// out0[j] = partial[0][j] + partial[1][j] + ... over `parts` lines of `cols`, in an order that only their number decides; out1
+// likewise from the lines behind those.  Either may be NULL.
+int ds_launch_sum_parts(const float *partial, int64_t parts, int64_t cols, float *out0, float *out1, hipStream_t stream);
