@@ -45,23 +45,33 @@ __device__ inline f32x4 mfma(u32x4 x, u32x4 y, f32x4 sum, __half) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), sum, 0, 0, 0);
 }
 
-__device__ inline float activation_any(float z, uint32_t act) {
-  switch (act) {
-    case DS_ACT_GELU: return activation<DS_ACT_GELU>(z);
-    case DS_ACT_GELU_TANH: return activation<DS_ACT_GELU_TANH>(z);
-    case DS_ACT_SILU: return activation<DS_ACT_SILU>(z);
-    default: return z;
-  }
+template <uint32_t ACT>
+__device__ inline void activate8(Eight &z) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) z.v[k] = activation<ACT>(z.v[k]);
+}
+
+// The first n <= 8 of eight biases from column j on, zeros where there is none.
+__device__ inline Eight bias8(const Epilogue &e, int64_t j, int n) { return get_up_to8_any(e.bias, e.bias_dtype, j, n, 0.f); }
+
+// The residual's bits of row i from column j on, n <= 8 of them, asked for long before they are used.
+struct Residual8 {
+  RowsOf<float>::Bits full;
+  RowsOf<__half>::Bits half;
+};
+__device__ inline Residual8 residual8(const Epilogue &e, int64_t i, int64_t j, int n) {
+  Residual8 r = {};
+  if (!e.residual.base) return r;
+  if (e.c_dtype == DS_F32) r.full = RowsOf<float>::ask(e.residual, i, j, n);
+  else r.half = RowsOf<__half>::ask(e.residual, i, j, n);
+  return r;
 }
 
 // Eight sums of row i from column j (a multiple of 8) on, n <= 8 of them in c, leave by the epilogue.  All lanes of the wavefront
 // take part, four neighbouring ones with a group of 32 columns.
-__device__ inline void finish8(const Epilogue &e, int64_t i, int64_t j, int n, Eight z) {
-  if (e.bias) {
-    const Eight b = get_up_to8_any(e.bias, e.bias_dtype, j, n, 0.f);
+__device__ inline void finish8(const Epilogue &e, int64_t i, int64_t j, int n, Eight z, const Eight &bias, const Residual8 &residual) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) z.v[k] += b.v[k];
-  }
+  for (int k = 0; k < 8; ++k) z.v[k] += bias.v[k];
   if (e.saved.base) {
     Eight s = z;
     if (n < 8) {
@@ -70,24 +80,26 @@ __device__ inline void finish8(const Epilogue &e, int64_t i, int64_t j, int n, E
     }
     mx8_put(e.saved, i, j, n, s);
   }
-  if (e.act != DS_ACT_NONE) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) z.v[k] = activation_any(z.v[k], e.act);
-  }
+  if (e.act == DS_ACT_GELU) activate8<DS_ACT_GELU>(z);
+  else if (e.act == DS_ACT_GELU_TANH) activate8<DS_ACT_GELU_TANH>(z);
+  else if (e.act == DS_ACT_SILU) activate8<DS_ACT_SILU>(z);
   if (n <= 0) return;
-  const int64_t at = i * e.c.stride + j, from = i * e.residual.stride + j;
-  const auto store = [&](auto type) {
+  const auto store = [&](auto type, const auto &bits) {
     typedef decltype(type) T;
     if (e.residual.base) {
-      const Eight r = get_up_to8<T>(e.residual.base, from, n);
+      const Eight r = Elem<T>::get8(&bits, 0);
 #pragma unroll
       for (int k = 0; k < 8; ++k) z.v[k] += r.v[k];
     }
-    put_up_to8<T>(e.c.base, at, n, z);
+    put_up_to8<T>(e.c.base, i * e.c.stride + j, n, z);
   };
-  if (e.c_dtype == DS_F32) store(float());
-  else if (e.c_dtype == DS_BF16) store(__hip_bfloat16());
-  else store(__half());
+  if (e.c_dtype == DS_F32) store(float(), residual.full);
+  else if (e.c_dtype == DS_BF16) store(__hip_bfloat16(), residual.half);
+  else store(__half(), residual.half);
+}
+__device__ inline int columns_of(const Epilogue &e, int64_t i, int64_t j) {
+  const int64_t left = i < e.m ? e.n - j : 0;
+  return (int)(left < 0 ? 0 : left < 8 ? left : 8);
 }
 
 constexpr int kTile = 64, kDeep = 32, kPitch = kDeep + 8;
@@ -167,11 +179,12 @@ __global__ __launch_bounds__(kThreads) void ds_matmul_kernel(Operand a, Operand 
   __syncthreads();
   for (int r = 0; r < 2; ++r) {
     const int row = r * 32 + threadIdx.x / 8, col = threadIdx.x % 8 * 8;
-    const int64_t i = p0 + row, j = q0 + col, left = i < e.m ? e.n - j : 0;
+    const int64_t i = p0 + row, j = q0 + col;
+    const int n = columns_of(e, i, j);
     Eight z;
 #pragma unroll
     for (int k = 0; k < 8; ++k) z.v[k] = lds.out[row][col + k];
-    finish8(e, i, j, (int)(left < 0 ? 0 : left < 8 ? left : 8), z);
+    finish8(e, i, j, n, z, bias8(e, j, n), residual8(e, i, j, n));
   }
 }
 
@@ -252,7 +265,8 @@ struct Stage {
   // step's first on, 0 and less where nothing is.
   __device__ inline void bring(int i, uint64_t from, int left, uint32_t lds, uint32_t spare, int wave) const {
     const int x = i * WAVES + wave;
-    const u32x4 resource = {(uint32_t)from, (uint32_t)(from >> 32), kNowhere, 0x00020000u};
+    const u32x4 resource = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)from), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(from >> 32)), kNowhere,
+                            0x00020000u};
     to_lds(kSpare == 0 || x < kTransfers ? lds + x * 1024 : spare, at_k[i] < left ? offset[i] : kNowhere, resource);
   }
   // The operand of a matrix instruction: 16 lines from p (a multiple of 16) on.
@@ -269,13 +283,15 @@ struct Stage {
 
 // Tiles of (WM * MI * 16) x (WN * NI * 16), a wavefront has MI * 16 rows of NI * 16 columns.  STAGES stages of LDS: while the matrix
 // instructions run on one, the transfers of the others are under way; one barrier a step.
-template <typename T, int MI, int NI, int WM, int WN, int STAGES, bool A_K, bool B_K>
+template <typename T, int MI, int NI, int WM, int WN, int STAGES, int EACH, bool A_K, bool B_K>
 __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs t, Epilogue e) {
   constexpr int kWaves = WM * WN, kM = WM * MI * 16, kN = WN * NI * 16;
   typedef Stage<kM, kWaves, A_K> A;
   typedef Stage<kN, kWaves, B_K> B;
   constexpr int kStage = A::kBytes + B::kBytes, kOutPitch = NI * 16 + 4;
-  static_assert(kWaves * 16 * kOutPitch * 4 <= STAGES * kStage, "the sums leave through the stages");
+  // of 16 rows of the sums each, as many as the stages' LDS holds for every wavefront: all, or half of them
+  constexpr int kOut = kWaves * MI * 16 * kOutPitch * 4 <= STAGES * kStage ? MI : MI / 2;
+  static_assert(kWaves * kOut * 16 * kOutPitch * 4 <= STAGES * kStage, "the sums leave through the stages");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES * kStage + (A::kSpare | B::kSpare)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -331,22 +347,30 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs
     }
   };
   const auto after = [](int stage) { return stage + 1 == STAGES ? 0 : stage + 1; };
+  constexpr int kAhead = STAGES - EACH + 1;  // steps whose transfers are under way before the first
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s)
+  for (int s = 0; s < kAhead; ++s)
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) bring(i, s);
-  stage_is_there<(STAGES - 2) * kLoads>();
+  stage_is_there<(kAhead - 1) * kLoads>();
 #pragma unroll
   for (int i = 0; i < MI + NI; ++i) fetch(even, lds, i);
-  // Two steps, s and s + 1, for a barrier: before them the operands of s are in registers, and the stages of s + 1 and s + 2 have to
-  // be there; those of s and before are free, for the transfers of s + STAGES - 1 and s + STAGES.  An odd last step's
-  // partner is zeros.
+  // A barrier for EACH steps.  Before the two steps s and s + 1 of one barrier the operands of s are in registers, and the stages
+  // of s + 1 and s + 2 have to be there; those of s and before are free, for the transfers of s + STAGES - 1 and s + STAGES.
+  // With a barrier for each step only the next stage has to be there.  An odd last step's partner is zeros.
   int at = 0;
   for (int64_t step = first; step < last; step += 2) {
-    stage_is_there<(STAGES - 4) * kLoads>();
     const int one = after(at), two = after(one);
-    advance(even, odd, one, at == 0 ? STAGES - 1 : at - 1);
-    advance(odd, even, two, at);
+    if (EACH == 2) {
+      stage_is_there<(STAGES - 4) * kLoads>();
+      advance(even, odd, one, at == 0 ? STAGES - 1 : at - 1);
+      advance(odd, even, two, at);
+    } else {
+      stage_is_there<(STAGES - 2) * kLoads>();
+      advance(even, odd, one, at);
+      stage_is_there<(STAGES - 2) * kLoads>();
+      advance(odd, even, two, one);
+    }
     at = two;
   }
   stage_is_there<0>();
@@ -367,22 +391,41 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs
     }
     return;
   }
-  float *out = (float *)lds + wave * 16 * kOutPitch;
+  // kRows of the wavefront's rows at a time go through LDS, and leave eight columns a lane, kBatch rows' residual asked for
+  // before the first of them is finished.
+  constexpr int kLanes = NI * 2, kPass = 64 / kLanes, kPasses = kOut * 16 / kPass, kBatch = kPasses % 4 == 0 ? 4 : kPasses % 3 == 0 ? 3 : kPasses % 2 == 0 ? 2 : 1;
+  static_assert(MI % kOut == 0 && kPasses % kBatch == 0, "whole batches");
+  float *out = (float *)lds + wave * kOut * 16 * kOutPitch;
+  const int col = lane % kLanes * 8;
+  const int64_t j = q0 + n0 + col;
+  const Eight bias = bias8(e, j, columns_of(e, 0, j));
 #pragma unroll
-  for (int i = 0; i < MI; ++i) {
+  for (int h = 0; h < MI / kOut; ++h) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) *(f32x4 *)(out + lane % 16 * kOutPitch + j * 16 + lane / 16 * 4) = sum[i][j];
+    for (int i = 0; i < kOut; ++i)
+#pragma unroll
+      for (int b = 0; b < NI; ++b) *(f32x4 *)(out + (i * 16 + lane % 16) * kOutPitch + b * 16 + lane / 16 * 4) = sum[h * kOut + i][b];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-    for (int r = 0; r < NI / 2; ++r) {
-      const int row = (r * 64 + lane) / (NI * 2), col = lane % (NI * 2) * 8;
-      Eight z;
-      const f32x4 lo = *(const f32x4 *)(out + row * kOutPitch + col), hi = *(const f32x4 *)(out + row * kOutPitch + col + 4);
+    for (int pass = 0; pass < kPasses; pass += kBatch) {
+      Residual8 residual[kBatch];
+      int n[kBatch];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) z.v[k] = lo[k], z.v[4 + k] = hi[k];
-      const int64_t at = p0 + m0 + i * 16 + row, j = q0 + n0 + col, left = at < e.m ? e.n - j : 0;
-      finish8(e, at, j, (int)(left < 0 ? 0 : left < 8 ? left : 8), z);
+      for (int u = 0; u < kBatch; ++u) {
+        const int64_t i = p0 + m0 + h * kOut * 16 + (pass + u) * kPass + lane / kLanes;
+        n[u] = columns_of(e, i, j);
+        residual[u] = residual8(e, i, j, n[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int row = (pass + u) * kPass + lane / kLanes;
+        Eight z;
+        const f32x4 lo = *(const f32x4 *)(out + row * kOutPitch + col), hi = *(const f32x4 *)(out + row * kOutPitch + col + 4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z.v[k] = lo[k], z.v[4 + k] = hi[k];
+        finish8(e, p0 + m0 + h * kOut * 16 + row, j, n[u], z, bias, residual[u]);
+      }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -392,15 +435,16 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs
 // The sums of the splits, in their order, and the epilogue.  A row has a multiple of four pieces of eight columns.
 __global__ __launch_bounds__(kThreads) void ds_matmul_join_kernel(const float *partial, uint32_t splits, uint32_t pieces, Epilogue e) {
   for (int64_t first = (int64_t)blockIdx.x * kThreads; first < e.m * pieces; first += (int64_t)gridDim.x * kThreads) {
-    const int64_t i = (first + threadIdx.x) / pieces, j = (first + threadIdx.x) % pieces * 8, left = i < e.m ? e.n - j : 0;
-    const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
+    const int64_t i = (first + threadIdx.x) / pieces, j = (first + threadIdx.x) % pieces * 8;
+    const int n = columns_of(e, i, j);
+    const Residual8 residual = residual8(e, i, j, n);
     Eight z = {};
     for (uint32_t s = 0; s < splits; ++s) {
       const Eight p = get_up_to8<float>(partial, (s * e.m + i) * e.n + j, n);
 #pragma unroll
       for (int k = 0; k < 8; ++k) z.v[k] += p.v[k];
     }
-    finish8(e, i, j, n, z);
+    finish8(e, i, j, n, z, bias8(e, j, n), residual);
   }
 }
 
@@ -499,13 +543,13 @@ int launch_lines(const Operand &o, int64_t depth, uint8_t *out, Source *s, hipSt
   return DS_OK;
 }
 
-template <typename T, int MI, int NI, int WM, int WN, int STAGES>
+template <typename T, int MI, int NI, int WM, int WN, int STAGES, int EACH>
 int launch_tile(const Operand &a, const Operand &b, const TileArgs &t, const Epilogue &e, hipStream_t stream) {
   const dim3 grid(t.tiles_m * t.tiles_n * t.splits), threads(WM * WN * 64);
-  if (a.k_last && b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, true, true>), grid, threads, 0, stream, t, e);
-  else if (a.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, true, false>), grid, threads, 0, stream, t, e);
-  else if (b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, false, true>), grid, threads, 0, stream, t, e);
-  else hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, false, false>), grid, threads, 0, stream, t, e);
+  if (a.k_last && b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, EACH, true, true>), grid, threads, 0, stream, t, e);
+  else if (a.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, EACH, true, false>), grid, threads, 0, stream, t, e);
+  else if (b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, EACH, false, true>), grid, threads, 0, stream, t, e);
+  else hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, EACH, false, false>), grid, threads, 0, stream, t, e);
   DS_HIP_TRY(hipGetLastError());
   return DS_OK;
 }
@@ -524,11 +568,11 @@ int launch_product(const Operand &a, const Operand &b, const Epilogue &e, int64_
   if (c.lines_a) DS_TRY(launch_lines<T>(a, depth, ws + c.at_a, &t.a, stream));
   if (c.lines_b) DS_TRY(launch_lines<T>(b, depth, ws + c.at_b, &t.b, stream));
   switch (c.tile) {
-    case 0: DS_TRY((launch_tile<T, 8, 4, 2, 4, 5>(a, b, t, e, stream))); break;
-    case 1: DS_TRY((launch_tile<T, 6, 4, 2, 4, 5>(a, b, t, e, stream))); break;
-    case 2: DS_TRY((launch_tile<T, 4, 4, 2, 4, 6>(a, b, t, e, stream))); break;
-    case 3: DS_TRY((launch_tile<T, 4, 4, 2, 2, 5>(a, b, t, e, stream))); break;
-    default: DS_TRY((launch_tile<T, 1, 4, 4, 1, 5>(a, b, t, e, stream))); break;
+    case 0: DS_TRY((launch_tile<T, 8, 4, 2, 4, 5, 2>(a, b, t, e, stream))); break;
+    case 1: DS_TRY((launch_tile<T, 6, 4, 2, 4, 5, 2>(a, b, t, e, stream))); break;
+    case 2: DS_TRY((launch_tile<T, 4, 4, 2, 4, 6, 2>(a, b, t, e, stream))); break;
+    case 3: DS_TRY((launch_tile<T, 4, 4, 2, 2, 5, 2>(a, b, t, e, stream))); break;
+    default: DS_TRY((launch_tile<T, 1, 4, 4, 1, 5, 2>(a, b, t, e, stream))); break;
   }
   if (c.splits == 1) return DS_OK;
   const int64_t pieces = ds_groups(e.n) * (kGroup / 8), groups = (e.m * pieces + kThreads - 1) / kThreads;
