@@ -190,7 +190,7 @@ __global__ __launch_bounds__(kThreads) void ds_matmul_kernel(Operand a, Operand 
 
 // ---- tiles whose operands go to LDS directly ---------------------------------------------------------------------
 
-constexpr int kStep = 32;  // of k: what one stage of LDS holds, and one matrix instruction takes
+constexpr int kStep = 64;  // of k: what a stage of LDS holds, twice what a matrix instruction takes
 
 // An operand as these kernels have it: 16-byte aligned, every line a whole number of 16-byte pieces apart and long.
 struct Source {
@@ -220,9 +220,10 @@ __device__ inline void stage_is_there() {
 }
 
 // The part of one operand that a work-group stages: P lines or columns, kStep of k.
-//   K_LAST: LDS holds P rows of 64 bytes, four pieces of eight k; piece c of row r is at c ^ turn_row(r).  A read takes 16 lanes
+//   K_LAST: LDS holds P rows of 128 bytes, eight pieces of eight k; piece c of row r is at c ^ (r % 8).  A read takes 16 lanes
 //     at a time, lanes 0-3, 12-15 and 20-27 first: rows 0-3 and 12-15 at one c and rows 4-11 at the next, which then lie in
-//     different banks.
+//     different banks.  (Rows of 64 bytes, so that a stage is half as deep, make twice the requests of the L2: 8192^3 in
+//     876 us, 958 so.)
 //   else: LDS holds kStep rows of P elements.  A lane's eight k are then in eight rows: ds_read_b64_tr_b16 reads four rows of 16
 //     elements with 16 lanes and gives each lane one column of them.  Pairs of pieces are exchanged by the row, so that
 //     the 32 lanes of a pass, eight rows of 32 bytes, meet every bank once.
@@ -234,7 +235,6 @@ struct Stage {
   static_assert(kBytes % 1024 == 0, "whole transfers");
   uint32_t offset[kLoads];  // of this lane's pieces from the operand's first element of the stage
   int at_k[kLoads];         // their place along k
-  static __device__ inline int turn_row(int r) { return (r >> 2 & 3) ^ (r >> 1 & 2); }
   static __device__ inline int turn(int k) {
     return P % 128 == 0 ? (k & 3) | (k >> 3 & 1) << 2 : (k >> 1 & 1) | (k >> 3 & 1) << 1;
   }
@@ -246,7 +246,7 @@ struct Stage {
       at_k[i] = 0, offset[i] = kNowhere;
       if (i * WAVES + wave >= kTransfers) continue;
       if (K_LAST) {
-        const int r = f / 4, c = (f % 4) ^ turn_row(r);
+        const int r = f / 8, c = (f % 8) ^ (r & 7);
         at_k[i] = c * 8;
         offset[i] = p0 + r < s.extent ? (uint32_t)(r * s.ld + c * 16) : kNowhere;
       } else {
@@ -269,28 +269,29 @@ struct Stage {
                             0x00020000u};
     to_lds(kSpare == 0 || x < kTransfers ? lds + x * 1024 : spare, at_k[i] < left ? offset[i] : kNowhere, resource);
   }
-  // The operand of a matrix instruction: 16 lines from p (a multiple of 16) on.
-  static __device__ inline u32x4 read(const uint8_t *lds, int p, int lane) {
-    if (K_LAST) return *(const u32x4 *)(lds + (p + lane % 16) * 64 + ((lane / 16) ^ turn_row(lane)) * 16);
+  // The operand of a matrix instruction: 16 lines from p (a multiple of 16) on, 32 of k from 32 * half on.
+  static __device__ inline u32x4 read(const uint8_t *lds, int p, int half, int lane) {
+    if (K_LAST) return *(const u32x4 *)(lds + (p + lane % 16) * 128 + ((half * 4 + lane / 16) ^ (lane & 7)) * 16);
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4 *Place;
-    const int k = lane / 16 * 8 + lane % 16 / 4;
+    const int k = half * 32 + lane / 16 * 8 + lane % 16 / 4;
     const uint8_t *at = lds + k * kLine + (((p / 16) ^ turn(k)) * 32) + lane % 4 * 8;
     const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)at), high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + 4 * kLine));
     return __builtin_bit_cast(u32x4, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
 
-// Tiles of (WM * MI * 16) x (WN * NI * 16), a wavefront has MI * 16 rows of NI * 16 columns.  STAGES stages of LDS: while the matrix
-// instructions run on one, the transfers of the others are under way; one barrier a step.
-template <typename T, int MI, int NI, int WM, int WN, int STAGES, int EACH, bool A_K, bool B_K>
+// Tiles of (WM * MI * 16) x (WN * NI * 16), a wavefront has MI * 16 rows of NI * 16 columns.  STAGES stages of LDS, and the
+// operands of two matrix instructions' k in registers: while those of one run, the other's come from LDS, and one stage is read
+// while the others are filled.
+template <typename T, int MI, int NI, int WM, int WN, int STAGES, bool A_K, bool B_K>
 __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs t, Epilogue e) {
   constexpr int kWaves = WM * WN, kM = WM * MI * 16, kN = WN * NI * 16;
   typedef Stage<kM, kWaves, A_K> A;
   typedef Stage<kN, kWaves, B_K> B;
   constexpr int kStage = A::kBytes + B::kBytes, kOutPitch = NI * 16 + 4;
-  // of 16 rows of the sums each, as many as the stages' LDS holds for every wavefront: all, or half of them
-  constexpr int kOut = kWaves * MI * 16 * kOutPitch * 4 <= STAGES * kStage ? MI : MI / 2;
+  // of 16 rows of the sums each, as many as the stages' LDS holds for every wavefront: all, a half or a quarter of them
+  constexpr int kRoom = STAGES * kStage / (kWaves * 16 * kOutPitch * 4), kOut = kRoom >= MI ? MI : kRoom >= MI / 2 ? MI / 2 : MI / 4;
   static_assert(kWaves * kOut * 16 * kOutPitch * 4 <= STAGES * kStage, "the sums leave through the stages");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES * kStage + (A::kSpare | B::kSpare)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -324,54 +325,46 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs
   struct Operands {
     u32x4 x[MI], y[NI];
   } even, odd;
-  const auto fetch = [&](Operands &o, const uint8_t *stage, int i) {
-    if (i < NI) o.y[i] = B::read(stage + A::kBytes, n0 + i * 16, lane);
-    else o.x[i - NI] = A::read(stage, m0 + (i - NI) * 16, lane);
+  const auto fetch = [&](Operands &o, const uint8_t *stage, int half, int i) {
+    if (i < NI) o.y[i] = B::read(stage + A::kBytes, n0 + i * 16, half, lane);
+    else o.x[i - NI] = A::read(stage, m0 + (i - NI) * 16, half, lane);
   };
-  // One step on the operands in `now`, while the next step's come from the stage `next_at` and a later step's go to the stage
-  // `to`.  Reads and transfers stand between the matrix instructions: a wavefront that starts all its transfers at once waits
-  // for the unit that takes them, 16 cycles for each.  (Transfers behind the last step bring zeros.)
-  const auto advance = [&](const Operands &now, Operands &next, int next_at, int to) {
+  // 32 of k on the operands in `now`, while the next 32's come from half `half` of the stage `next_at`; with the first half a later
+  // step's transfers to the stage `to` start.  Reads and transfers stand between the matrix instructions: a wavefront that
+  // starts all its transfers at once waits for the unit that takes them, 16 cycles for each.  (Transfers behind the last step
+  // bring zeros.)
+  const auto advance = [&](const Operands &now, Operands &next, int next_at, auto half, int to) {
     const uint8_t *stage = lds + next_at * kStage;
     int read = 0, brought = 0;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       // (MI + NI) reads and kLoads transfers in as many parts as there are rows
 #pragma unroll
-      for (; read < (MI + NI) * (i + 1) / MI; ++read) fetch(next, stage, read);
+      for (; read < (MI + NI) * (i + 1) / MI; ++read) fetch(next, stage, half, read);
 #pragma unroll
-      for (; brought < kLoads * (i + 1) / MI; ++brought) bring(brought, to);
+      for (; half == 0 && brought < kLoads * (i + 1) / MI; ++brought) bring(brought, to);
 #pragma unroll
       for (int j = 0; j < NI; ++j) sum[i][j] = mfma(now.y[j], now.x[i], sum[i][j], T());
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   const auto after = [](int stage) { return stage + 1 == STAGES ? 0 : stage + 1; };
-  constexpr int kAhead = STAGES - EACH + 1;  // steps whose transfers are under way before the first
 #pragma unroll
-  for (int s = 0; s < kAhead; ++s)
+  for (int s = 0; s < STAGES; ++s)
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) bring(i, s);
-  stage_is_there<(kAhead - 1) * kLoads>();
+  stage_is_there<(STAGES - 1) * kLoads>();
 #pragma unroll
-  for (int i = 0; i < MI + NI; ++i) fetch(even, lds, i);
-  // A barrier for EACH steps.  Before the two steps s and s + 1 of one barrier the operands of s are in registers, and the stages
-  // of s + 1 and s + 2 have to be there; those of s and before are free, for the transfers of s + STAGES - 1 and s + STAGES.
-  // With a barrier for each step only the next stage has to be there.  An odd last step's partner is zeros.
+  for (int i = 0; i < MI + NI; ++i) fetch(even, lds, 0, i);
+  // One barrier a step.  Behind it everybody has the step's second half in registers, so that its stage is free for the step
+  // STAGES further on, and the next step's stage is there.
   int at = 0;
-  for (int64_t step = first; step < last; step += 2) {
-    const int one = after(at), two = after(one);
-    if (EACH == 2) {
-      stage_is_there<(STAGES - 4) * kLoads>();
-      advance(even, odd, one, at == 0 ? STAGES - 1 : at - 1);
-      advance(odd, even, two, at);
-    } else {
-      stage_is_there<(STAGES - 2) * kLoads>();
-      advance(even, odd, one, at);
-      stage_is_there<(STAGES - 2) * kLoads>();
-      advance(odd, even, two, one);
-    }
-    at = two;
+  for (int64_t step = first; step < last; ++step) {
+    const int next = after(at);
+    advance(even, odd, at, std::integral_constant<int, 1>(), 0);
+    stage_is_there<(STAGES - 2) * kLoads>();
+    advance(odd, even, next, std::integral_constant<int, 0>(), at);
+    at = next;
   }
   stage_is_there<0>();
   // a lane's sums: row lane % 16 of the 16, columns 16 j + 4 (lane / 16) and on
@@ -543,13 +536,13 @@ int launch_lines(const Operand &o, int64_t depth, uint8_t *out, Source *s, hipSt
   return DS_OK;
 }
 
-template <typename T, int MI, int NI, int WM, int WN, int STAGES, int EACH>
+template <typename T, int MI, int NI, int WM, int WN, int STAGES>
 int launch_tile(const Operand &a, const Operand &b, const TileArgs &t, const Epilogue &e, hipStream_t stream) {
   const dim3 grid(t.tiles_m * t.tiles_n * t.splits), threads(WM * WN * 64);
-  if (a.k_last && b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, EACH, true, true>), grid, threads, 0, stream, t, e);
-  else if (a.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, EACH, true, false>), grid, threads, 0, stream, t, e);
-  else if (b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, EACH, false, true>), grid, threads, 0, stream, t, e);
-  else hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, EACH, false, false>), grid, threads, 0, stream, t, e);
+  if (a.k_last && b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, true, true>), grid, threads, 0, stream, t, e);
+  else if (a.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, true, false>), grid, threads, 0, stream, t, e);
+  else if (b.k_last) hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, false, true>), grid, threads, 0, stream, t, e);
+  else hipLaunchKernelGGL((ds_matmul_tile_kernel<T, MI, NI, WM, WN, STAGES, false, false>), grid, threads, 0, stream, t, e);
   DS_HIP_TRY(hipGetLastError());
   return DS_OK;
 }
@@ -568,11 +561,11 @@ int launch_product(const Operand &a, const Operand &b, const Epilogue &e, int64_
   if (c.lines_a) DS_TRY(launch_lines<T>(a, depth, ws + c.at_a, &t.a, stream));
   if (c.lines_b) DS_TRY(launch_lines<T>(b, depth, ws + c.at_b, &t.b, stream));
   switch (c.tile) {
-    case 0: DS_TRY((launch_tile<T, 8, 4, 2, 4, 5, 2>(a, b, t, e, stream))); break;
-    case 1: DS_TRY((launch_tile<T, 6, 4, 2, 4, 5, 2>(a, b, t, e, stream))); break;
-    case 2: DS_TRY((launch_tile<T, 4, 4, 2, 4, 6, 2>(a, b, t, e, stream))); break;
-    case 3: DS_TRY((launch_tile<T, 4, 4, 2, 2, 5, 2>(a, b, t, e, stream))); break;
-    default: DS_TRY((launch_tile<T, 1, 4, 4, 1, 5, 2>(a, b, t, e, stream))); break;
+    case 0: DS_TRY((launch_tile<T, 8, 4, 2, 4, 2>(a, b, t, e, stream))); break;
+    case 1: DS_TRY((launch_tile<T, 6, 4, 2, 4, 2>(a, b, t, e, stream))); break;
+    case 2: DS_TRY((launch_tile<T, 4, 4, 2, 4, 3>(a, b, t, e, stream))); break;
+    case 3: DS_TRY((launch_tile<T, 4, 4, 2, 2, 2>(a, b, t, e, stream))); break;
+    default: DS_TRY((launch_tile<T, 1, 4, 4, 1, 5>(a, b, t, e, stream))); break;
   }
   if (c.splits == 1) return DS_OK;
   const int64_t pieces = ds_groups(e.n) * (kGroup / 8), groups = (e.m * pieces + kThreads - 1) / kThreads;
