@@ -54,22 +54,10 @@ __device__ inline void activate8(Eight &z) {
 // The first n <= 8 of eight biases from column j on, zeros where there is none.
 __device__ inline Eight bias8(const Epilogue &e, int64_t j, int n) { return get_up_to8_any(e.bias, e.bias_dtype, j, n, 0.f); }
 
-// The residual's bits of row i from column j on, n <= 8 of them, asked for long before they are used.
-struct Residual8 {
-  RowsOf<float>::Bits full;
-  RowsOf<__half>::Bits half;
-};
-__device__ inline Residual8 residual8(const Epilogue &e, int64_t i, int64_t j, int n) {
-  Residual8 r = {};
-  if (!e.residual.base) return r;
-  if (e.c_dtype == DS_F32) r.full = RowsOf<float>::ask(e.residual, i, j, n);
-  else r.half = RowsOf<__half>::ask(e.residual, i, j, n);
-  return r;
-}
-
-// Eight sums of row i from column j (a multiple of 8) on, n <= 8 of them in c, leave by the epilogue.  All lanes of the wavefront
-// take part, four neighbouring ones with a group of 32 columns.
-__device__ inline void finish8(const Epilogue &e, int64_t i, int64_t j, int n, Eight z, const Eight &bias, const Residual8 &residual) {
+// Eight sums of row i from column j (a multiple of 8) on, n <= 8 of them in c, leave by the epilogue; T: c's type.  All lanes of the
+// wavefront take part, four neighbouring ones with a group of 32 columns.  The residual's bits have been asked for before.
+template <typename T>
+__device__ inline void finish8(const Epilogue &e, int64_t i, int64_t j, int n, Eight z, const Eight &bias, const typename RowsOf<T>::Bits &residual) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) z.v[k] += bias.v[k];
   if (e.saved.base) {
@@ -84,18 +72,24 @@ __device__ inline void finish8(const Epilogue &e, int64_t i, int64_t j, int n, E
   else if (e.act == DS_ACT_GELU_TANH) activate8<DS_ACT_GELU_TANH>(z);
   else if (e.act == DS_ACT_SILU) activate8<DS_ACT_SILU>(z);
   if (n <= 0) return;
-  const auto store = [&](auto type, const auto &bits) {
-    typedef decltype(type) T;
-    if (e.residual.base) {
-      const Eight r = Elem<T>::get8(&bits, 0);
+  if (e.residual.base) {
+    const Eight r = RowsOf<T>::value(residual, 8);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) z.v[k] += r.v[k];
-    }
-    put_up_to8<T>(e.c.base, i * e.c.stride + j, n, z);
-  };
-  if (e.c_dtype == DS_F32) store(float(), residual.full);
-  else if (e.c_dtype == DS_BF16) store(__hip_bfloat16(), residual.half);
-  else store(__half(), residual.half);
+    for (int k = 0; k < 8; ++k) z.v[k] += r.v[k];
+  }
+  put_up_to8<T>(e.c.base, i * e.c.stride + j, n, z);
+}
+template <typename T>
+__device__ inline typename RowsOf<T>::Bits residual8(const Epilogue &e, int64_t i, int64_t j, int n) {
+  typename RowsOf<T>::Bits r = {};
+  if (e.residual.base) r = RowsOf<T>::ask(e.residual, i, j, n);
+  return r;
+}
+template <typename F>
+__device__ inline void with_c_type(const Epilogue &e, F f) {
+  if (e.c_dtype == DS_F32) f(float());
+  else if (e.c_dtype == DS_BF16) f(__hip_bfloat16());
+  else f(__half());
 }
 __device__ inline int columns_of(const Epilogue &e, int64_t i, int64_t j) {
   const int64_t left = i < e.m ? e.n - j : 0;
@@ -177,15 +171,18 @@ __global__ __launch_bounds__(kThreads) void ds_matmul_kernel(Operand a, Operand 
 #pragma unroll
   for (int t = 0; t < 4; ++t) *(f32x4 *)&lds.out[wave * 16 + lane % 16][t * 16 + lane / 16 * 4] = sum[t];
   __syncthreads();
-  for (int r = 0; r < 2; ++r) {
-    const int row = r * 32 + threadIdx.x / 8, col = threadIdx.x % 8 * 8;
-    const int64_t i = p0 + row, j = q0 + col;
-    const int n = columns_of(e, i, j);
-    Eight z;
+  with_c_type(e, [&](auto type) {
+    typedef decltype(type) C;
+    for (int r = 0; r < 2; ++r) {
+      const int row = r * 32 + threadIdx.x / 8, col = threadIdx.x % 8 * 8;
+      const int64_t i = p0 + row, j = q0 + col;
+      const int n = columns_of(e, i, j);
+      Eight z;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) z.v[k] = lds.out[row][col + k];
-    finish8(e, i, j, n, z, bias8(e, j, n), residual8(e, i, j, n));
-  }
+      for (int k = 0; k < 8; ++k) z.v[k] = lds.out[row][col + k];
+      finish8<C>(e, i, j, n, z, bias8(e, j, n), residual8<C>(e, i, j, n));
+    }
+  });
 }
 
 // ---- tiles whose operands go to LDS directly ---------------------------------------------------------------------
@@ -289,10 +286,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs
   constexpr int kWaves = WM * WN, kM = WM * MI * 16, kN = WN * NI * 16;
   typedef Stage<kM, kWaves, A_K> A;
   typedef Stage<kN, kWaves, B_K> B;
-  constexpr int kStage = A::kBytes + B::kBytes, kOutPitch = NI * 16 + 4;
-  // of 16 rows of the sums each, as many as the stages' LDS holds for every wavefront: all, a half or a quarter of them
-  constexpr int kRoom = STAGES * kStage / (kWaves * 16 * kOutPitch * 4), kOut = kRoom >= MI ? MI : kRoom >= MI / 2 ? MI / 2 : MI / 4;
-  static_assert(kWaves * kOut * 16 * kOutPitch * 4 <= STAGES * kStage, "the sums leave through the stages");
+  constexpr int kStage = A::kBytes + B::kBytes, kOutPitch = NI * 16;
+  // of 16 rows of the sums each, as many as the stages' LDS holds for every wavefront: all, or half of them
+  constexpr int kRoom = STAGES * kStage / (kWaves * 16 * kOutPitch * 4), kOut = kRoom >= MI ? MI : MI / 2;
+  static_assert(NI == 4 && kWaves * kOut * 16 * kOutPitch * 4 <= STAGES * kStage, "the sums leave through the stages");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES * kStage + (A::kSpare | B::kSpare)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -333,16 +330,21 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs
   // step's transfers to the stage `to` start.  Reads and transfers stand between the matrix instructions: a wavefront that
   // starts all its transfers at once waits for the unit that takes them, 16 cycles for each.  (Transfers behind the last step
   // bring zeros.)
+  constexpr int kQuiet = MI / 8;
   const auto advance = [&](const Operands &now, Operands &next, int next_at, auto half, int to) {
     const uint8_t *stage = lds + next_at * kStage;
+    // rows of matrix instructions in front of the barrier, with it, and behind the last read
+    constexpr int kFirst = half == 0 ? kQuiet : 0, kReading = MI - kFirst - kQuiet;
     int read = 0, brought = 0;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      // (MI + NI) reads and kLoads transfers in as many parts as there are rows
+      if (half == 0 && i == kFirst) stage_is_there<(STAGES - 2) * kLoads>();
+      if (i >= kFirst) {
 #pragma unroll
-      for (; read < (MI + NI) * (i + 1) / MI; ++read) fetch(next, stage, half, read);
+        for (; read < MI + NI && read * kReading < (MI + NI) * (i + 1 - kFirst); ++read) fetch(next, stage, half, read);
 #pragma unroll
-      for (; half == 0 && brought < kLoads * (i + 1) / MI; ++brought) bring(brought, to);
+        for (; half == 0 && brought * (MI - kFirst) < kLoads * (i + 1 - kFirst); ++brought) bring(brought, to);
+      }
 #pragma unroll
       for (int j = 0; j < NI; ++j) sum[i][j] = mfma(now.y[j], now.x[i], sum[i][j], T());
       __builtin_amdgcn_sched_barrier(0);
@@ -362,7 +364,6 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs
   for (int64_t step = first; step < last; ++step) {
     const int next = after(at);
     advance(even, odd, at, std::integral_constant<int, 1>(), 0);
-    stage_is_there<(STAGES - 2) * kLoads>();
     advance(odd, even, next, std::integral_constant<int, 0>(), at);
     at = next;
   }
@@ -390,62 +391,87 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs
   static_assert(MI % kOut == 0 && kPasses % kBatch == 0, "whole batches");
   float *out = (float *)lds + wave * kOut * 16 * kOutPitch;
   const int col = lane % kLanes * 8;
+  // four floats, their place in a row exchanged by the row, so that 16 rows' are in different banks
+  const auto piece = [](int row, int at) { return (at ^ (row & 15)) * 4; };
   const int64_t j = q0 + n0 + col;
   const Eight bias = bias8(e, j, columns_of(e, 0, j));
-#pragma unroll
-  for (int h = 0; h < MI / kOut; ++h) {
-#pragma unroll
-    for (int i = 0; i < kOut; ++i)
-#pragma unroll
-      for (int b = 0; b < NI; ++b) *(f32x4 *)(out + (i * 16 + lane % 16) * kOutPitch + b * 16 + lane / 16 * 4) = sum[h * kOut + i][b];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+  // (The registers that hold the sums are named in the code, so each part's way to LDS is written out; the rest is one loop.)
+  const auto leave = [&](auto type, auto whole) {
+    typedef decltype(type) C;
 #pragma unroll 1
-    for (int pass = 0; pass < kPasses; pass += kBatch) {
-      Residual8 residual[kBatch];
-      int n[kBatch];
+    for (int h = 0; h < MI / kOut; ++h) {
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int64_t i = p0 + m0 + h * kOut * 16 + (pass + u) * kPass + lane / kLanes;
-        n[u] = columns_of(e, i, j);
-        residual[u] = residual8(e, i, j, n[u]);
+      for (int part = 0; part < MI / kOut; ++part)
+        if (h == part) {
+#pragma unroll
+          for (int i = 0; i < kOut; ++i)
+#pragma unroll
+            for (int b = 0; b < NI; ++b) *(f32x4 *)(out + (i * 16 + lane % 16) * kOutPitch + piece(lane, b * 4 + lane / 16)) = sum[part * kOut + i][b];
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+      for (int pass = 0; pass < kPasses; pass += kBatch) {
+        typename RowsOf<C>::Bits residual[kBatch];
+        const int64_t row0 = p0 + m0 + h * kOut * 16 + pass * kPass + lane / kLanes;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) residual[u] = residual8<C>(e, row0 + u * kPass, j, whole ? 8 : columns_of(e, row0 + u * kPass, j));
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int row = (pass + u) * kPass + lane / kLanes;
+          Eight z;
+          const f32x4 lo = *(const f32x4 *)(out + row * kOutPitch + piece(row, col / 4)), hi = *(const f32x4 *)(out + row * kOutPitch + piece(row, col / 4 + 1));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) z.v[k] = lo[k], z.v[4 + k] = hi[k];
+          finish8<C>(e, row0 + u * kPass, j, whole ? 8 : columns_of(e, row0 + u * kPass, j), z, bias, residual[u]);
+        }
       }
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int row = (pass + u) * kPass + lane / kLanes;
-        Eight z;
-        const f32x4 lo = *(const f32x4 *)(out + row * kOutPitch + col), hi = *(const f32x4 *)(out + row * kOutPitch + col + 4);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) z.v[k] = lo[k], z.v[4 + k] = hi[k];
-        finish8(e, p0 + m0 + h * kOut * 16 + row, j, n[u], z, bias, residual[u]);
-      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
+  };
+  with_c_type(e, [&](auto type) {
+    if (p0 + kM <= e.m && q0 + kN <= e.n) leave(type, std::true_type());
+    else leave(type, std::false_type());
+  });
 }
 
 // The sums of the splits, in their order, and the epilogue.  A row has a multiple of four pieces of eight columns.
+template <typename C, typename Index>
 __global__ __launch_bounds__(kThreads) void ds_matmul_join_kernel(const float *partial, uint32_t splits, uint32_t pieces, Epilogue e) {
   for (int64_t first = (int64_t)blockIdx.x * kThreads; first < e.m * pieces; first += (int64_t)gridDim.x * kThreads) {
-    const int64_t i = (first + threadIdx.x) / pieces, j = (first + threadIdx.x) % pieces * 8;
+    const Index item = (Index)(first + threadIdx.x), row = item / (Index)pieces;
+    const int64_t i = row, j = (int64_t)(item - row * (Index)pieces) * 8;
     const int n = columns_of(e, i, j);
-    const Residual8 residual = residual8(e, i, j, n);
+    const auto residual = residual8<C>(e, i, j, n);
+    const float *from = partial + i * e.n + j;
+    const int64_t apart = e.m * e.n;
     Eight z = {};
-    for (uint32_t s = 0; s < splits; ++s) {
-      const Eight p = get_up_to8<float>(partial, (s * e.m + i) * e.n + j, n);
+    uint32_t s = 0;
+    for (; s + 4 <= splits; s += 4, from += 4 * apart) {  // four at a time on their way
+      Eight p[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) p[u] = get_up_to8<float>(from, u * apart, n);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) z.v[k] += p[u].v[k];
+    }
+    for (; s < splits; ++s, from += apart) {
+      const Eight p = get_up_to8<float>(from, 0, n);
 #pragma unroll
       for (int k = 0; k < 8; ++k) z.v[k] += p.v[k];
     }
-    finish8(e, i, j, n, z, bias8(e, j, n), residual);
+    finish8<C>(e, i, j, n, z, bias8(e, j, n), residual);
   }
 }
 
 // An operand's lines of `length` elements as lines of 16-bit values, a multiple of eight of them, the rest zeros.
-template <typename T>
+template <typename T, typename Index>
 __global__ __launch_bounds__(kThreads) void ds_matmul_lines_kernel(Operand o, int64_t lines, int64_t length, uint16_t *out, uint32_t pieces) {
   for (int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x; at < lines * pieces; at += (int64_t)gridDim.x * kThreads) {
-    const int64_t line = at / pieces, j = at % pieces * 8;
+    const Index line = (Index)at / (Index)pieces;
+    const int64_t j = (int64_t)((Index)at - line * (Index)pieces) * 8;
     *(u32x4 *)(out + at * 8) = o.k_last ? bring8<T>(o, line, j, length) : bring8<T>(o, j, line, lines);
   }
 }
@@ -524,13 +550,31 @@ Choice choose(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t 
   return c;
 }
 
+int launch_join(const float *partial, uint32_t splits, const Epilogue &e, hipStream_t stream) {
+  const int64_t pieces = ds_groups(e.n) * (kGroup / 8), groups = (e.m * pieces + kThreads - 1) / kThreads;
+  return ds_with_type(e.c_dtype, [&](auto type) -> int {
+    typedef decltype(type) C;
+    const auto launch = [&](auto kernel) -> int {
+      hipLaunchKernelGGL(kernel, dim3((uint32_t)(groups < kMaxGrid ? groups : kMaxGrid)), dim3(kThreads), 0, stream, partial, splits,
+                         (uint32_t)pieces, e);
+      DS_HIP_TRY(hipGetLastError());
+      return DS_OK;
+    };
+    return groups <= (int64_t)0xffffffff / kThreads ? launch(ds_matmul_join_kernel<C, uint32_t>) : launch(ds_matmul_join_kernel<C, uint64_t>);
+  });
+}
+
 template <typename T>
 int launch_lines(const Operand &o, int64_t depth, uint8_t *out, Source *s, hipStream_t stream) {
   const int64_t lines = o.k_last ? o.extent : depth, length = o.k_last ? depth : o.extent, pieces = (length + 7) / 8;
   const int64_t groups = (lines * pieces + kThreads - 1) / kThreads;
-  hipLaunchKernelGGL(ds_matmul_lines_kernel<T>, dim3((uint32_t)(groups < kMaxGrid ? groups : kMaxGrid)), dim3(kThreads), 0, stream, o, lines,
-                     length, (uint16_t *)out, (uint32_t)pieces);
-  DS_HIP_TRY(hipGetLastError());
+  const auto launch = [&](auto kernel) -> int {
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(groups < kMaxGrid ? groups : kMaxGrid)), dim3(kThreads), 0, stream, o, lines, length,
+                       (uint16_t *)out, (uint32_t)pieces);
+    DS_HIP_TRY(hipGetLastError());
+    return DS_OK;
+  };
+  DS_TRY(groups <= (int64_t)0xffffffff / kThreads ? launch(ds_matmul_lines_kernel<T, uint32_t>) : launch(ds_matmul_lines_kernel<T, uint64_t>));
   // (the zeros behind a line of p are columns of no output)
   *s = Source{out, pieces * 16, o.k_last ? o.extent : pieces * 8};
   return DS_OK;
@@ -568,11 +612,7 @@ int launch_product(const Operand &a, const Operand &b, const Epilogue &e, int64_
     default: DS_TRY((launch_tile<T, 1, 4, 4, 1, 5>(a, b, t, e, stream))); break;
   }
   if (c.splits == 1) return DS_OK;
-  const int64_t pieces = ds_groups(e.n) * (kGroup / 8), groups = (e.m * pieces + kThreads - 1) / kThreads;
-  hipLaunchKernelGGL(ds_matmul_join_kernel, dim3((uint32_t)(groups < kMaxGrid ? groups : kMaxGrid)), dim3(kThreads), 0, stream, t.partial,
-                     t.splits, (uint32_t)pieces, e);
-  DS_HIP_TRY(hipGetLastError());
-  return DS_OK;
+  return launch_join(t.partial, t.splits, e, stream);
 }
 
 }  // namespace

@@ -68,6 +68,10 @@ inline int ds_with_type(uint32_t dtype, F f) {
 typedef uint32_t ds_u32x2 __attribute__((ext_vector_type(2), aligned(1)));
 typedef uint32_t ds_u32x4 __attribute__((ext_vector_type(4), aligned(1)));
 
+typedef float ds_f32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 ds_bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 ds_f16x8 __attribute__((ext_vector_type(8)));
+
 // Eight elements as 32-bit floats.
 struct Eight {
   float v[8];
@@ -115,10 +119,7 @@ struct Elem<__hip_bfloat16> {
     return e;
   }
   static __device__ inline void put8(void *p, int64_t i, const Eight &e) {
-    ds_u32x4 a;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] = float_to_bf16(e.v[2 * k]) | float_to_bf16(e.v[2 * k + 1]) << 16;
-    *(ds_u32x4 *)((uint16_t *)p + i) = a;
+    *(ds_u32x4 *)((uint16_t *)p + i) = __builtin_bit_cast(ds_u32x4, __builtin_convertvector(__builtin_bit_cast(ds_f32x8, e), ds_bf16x8));
   }
 };
 template <>
@@ -133,10 +134,7 @@ struct Elem<__half> {
     return e;
   }
   static __device__ inline void put8(void *p, int64_t i, const Eight &e) {
-    ds_u32x4 a;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] = float_to_f16(e.v[2 * k]) | float_to_f16(e.v[2 * k + 1]) << 16;
-    *(ds_u32x4 *)((uint16_t *)p + i) = a;
+    *(ds_u32x4 *)((uint16_t *)p + i) = __builtin_bit_cast(ds_u32x4, __builtin_convertvector(__builtin_bit_cast(ds_f32x8, e), ds_f16x8));
   }
 };
 
