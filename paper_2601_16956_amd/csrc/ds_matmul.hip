@@ -476,6 +476,118 @@ __global__ __launch_bounds__(kThreads) void ds_matmul_lines_kernel(Operand o, in
   }
 }
 
+// ---- few rows of a, and a weight [out, in] -------------------------------------------------------------------------
+
+// At most 16 rows: what counts is reading b once, at the rate of HBM.  A work-group of eight wavefronts has 32 columns of c; a wavefront
+// takes every eighth piece of 64 k, so that neighbouring wavefronts read neighbouring lines, and asks for the next four pieces
+// before it multiplies these.  A lane reads 32 neighbouring bytes of a line of b, two matrix instructions' operands: the order of k within
+// a piece is any, as long as a's is the same.  The wavefronts' sums are added in their order, in LDS.
+constexpr int kFewRows = 16, kFewCols = 32, kFewWaves = 8;
+
+// Eight neighbouring k of line p from k on; what is beyond the matrix is 0.
+__device__ inline u32x4 line8(const Operand &o, int64_t p, int64_t k, int64_t depth) {
+  u32x4 r = {0, 0, 0, 0};
+  if (p >= o.extent) return r;
+  const uint16_t *q = (const uint16_t *)o.base + p * o.ld + k;
+  if (k + 8 <= depth) return *(const ds_u32x4 *)q;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (k + i < depth) r[i / 2] |= (uint32_t)q[i] << (16 * (i % 2));
+  return r;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kFewWaves * 64) void ds_matmul_few_kernel(Operand a, Operand b, Epilogue e, int64_t depth) {
+  constexpr int kPieces = 4;
+  __shared__ float sums[kFewWaves][kFewRows][kFewCols + 4];
+  __shared__ float out[kFewRows][kFewCols + 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, line = lane % 16;
+  const int64_t q0 = (int64_t)blockIdx.x * kFewCols;
+  f32x4 sum[2] = {};
+  struct Piece {
+    u32x4 w[2][2], x[2];
+  };
+  // lines beyond the matrix read its last one, and lead to sums that nobody stores
+  const uint16_t *from_w[2], *from_x;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int64_t p = q0 + s * 16 + line;
+    from_w[s] = (const uint16_t *)b.base + (p < b.extent ? p : b.extent - 1) * b.ld + lane / 16 * 16;
+  }
+  from_x = (const uint16_t *)a.base + (line < a.extent ? line : a.extent - 1) * a.ld + lane / 16 * 16;
+  const auto ask = [&](Piece &p, int64_t k) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) p.w[s][h] = *(const ds_u32x4 *)(from_w[s] + k + h * 8);
+      p.x[h] = *(const ds_u32x4 *)(from_x + k + h * 8);
+    }
+  };
+  const auto multiply = [&](const Piece &p) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) sum[s] = mfma(p.w[s][h], p.x[h], sum[s], T());
+  };
+  constexpr int64_t kApart = kFewWaves * 64;
+  // this wavefront's whole pieces, the first `fours` of them four at a time
+  const int64_t whole = depth / 64, mine = whole > wave ? (whole - wave + kFewWaves - 1) / kFewWaves : 0, fours = mine / kPieces;
+  int64_t k = wave * 64;
+  if (fours > 0) {
+    Piece now[kPieces], next[kPieces];
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u) ask(now[u], k + u * kApart);
+    for (int64_t f = 1; f < fours; ++f) {
+      k += kPieces * kApart;
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u) ask(next[u], k + u * kApart);
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u) multiply(now[u]), now[u] = next[u];
+    }
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u) multiply(now[u]);
+    k += kPieces * kApart;
+  }
+  for (int64_t f = fours * kPieces; f < mine; ++f, k += kApart) {
+    Piece p;
+    ask(p, k);
+    multiply(p);
+  }
+  if (depth % 64 != 0 && whole % kFewWaves == wave) {  // the rest of k
+    Piece p;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t at = whole * 64 + lane / 16 * 16 + h * 8;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) p.w[s][h] = line8(b, q0 + s * 16 + line, at, depth);
+      p.x[h] = line8(a, line, at, depth);
+    }
+    multiply(p);
+  }
+  // a lane's sums: row lane % 16, columns 16 s + 4 (lane / 16) and on
+#pragma unroll
+  for (int s = 0; s < 2; ++s) *(f32x4 *)&sums[wave][line][s * 16 + lane / 16 * 4] = sum[s];
+  __syncthreads();
+  if (threadIdx.x < kFewRows * kFewCols) {
+    const int i = threadIdx.x / kFewCols, j = threadIdx.x % kFewCols;
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) total += sums[w][i][j];
+    out[i][j] = total;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  with_c_type(e, [&](auto type) {
+    typedef decltype(type) C;
+    const int64_t i = lane / 4, j = q0 + lane % 4 * 8;
+    const int n = columns_of(e, i, j);
+    Eight z;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) z.v[k] = out[i][lane % 4 * 8 + k];
+    finish8<C>(e, i, j, n, z, bias8(e, j, n), residual8<C>(e, i, j, n));
+  });
+}
+
 // a (or b's transpose): p along `along` = its rows if `p_rows`.
 Operand operand(const ds_matrix *m, bool p_rows) {
   const int64_t p = p_rows ? m->rows : m->cols, k = p_rows ? m->cols : m->rows;
@@ -501,7 +613,7 @@ int check_product(const ds_matrix *a, const ds_matrix *b, const ds_matrix *c) {
 
 // ---- how a product is computed ---------------------------------------------------------------------------------------
 
-enum class Way { kSimple, kTile };
+enum class Way { kSimple, kTile, kFew };
 struct Choice {
   Way way;
   int tile;         // index into kTiles
@@ -509,10 +621,29 @@ struct Choice {
   bool lines_a, lines_b;  // is the operand laid out in the workspace first?
   uint64_t at_a, at_b, at_partial, bytes;
 };
+// A tile's extents, how many of its work-groups a CU holds, and what they take, in us: before and behind the steps; a step where most
+// CUs are idle; a step with 1, 2, 3 work-groups on every CU.  (Measured with bfloat16 [out, in] on products of 4 to 256 steps; what
+// the steps take on a full chip is decided by its power.)
 struct TileSize {
-  int m, n, at_once;  // at_once: work-groups on a CU
+  int m, n, at_once;
+  double around, idle, step[3];
 };
-constexpr TileSize kTiles[] = {{256, 256, 1}, {192, 256, 1}, {128, 256, 1}, {128, 128, 2}, {64, 64, 4}};
+constexpr TileSize kTiles[] = {
+    {256, 256, 1, 9.9, 0.96, {1.41}},       {192, 256, 1, 8.6, 0.78, {1.20}},
+    {128, 256, 1, 7.1, 0.56, {0.80}},       {128, 128, 1, 5.6, 0.36, {0.55}},
+    {64, 128, 2, 5.2, 0.295, {0.33, 0.66}}, {64, 64, 3, 4.7, 0.255, {0.27, 0.36, 0.70}},
+};
+constexpr int64_t kCus = 256;
+double tile_time(const TileSize &s, int64_t m, int64_t n, int64_t steps, int64_t splits) {
+  const int64_t groups = (m + s.m - 1) / s.m * ((n + s.n - 1) / s.n) * splits, each = (steps + splits - 1) / splits;
+  const int64_t on_cu = (groups + kCus - 1) / kCus, rounds = (on_cu + s.at_once - 1) / s.at_once, rest = on_cu % s.at_once;
+  double step = (double)(on_cu / s.at_once) * s.step[s.at_once - 1] + (rest ? s.step[rest - 1] : 0.0);
+  if (on_cu == 1) step = s.idle + (s.step[0] - s.idle) * (double)groups / kCus;
+  // a further round's beginning and end; those of work-groups that share a CU overlap
+  double t = s.around + (double)each * step + (double)(rounds - 1) * (s.around - 3.0);
+  if (splits > 1) t += 4.0 + (double)m * (double)n * (double)splits * 8.0 / 5e6;  // the sums' way through memory, and a launch
+  return t;
+}
 
 // May the operand be read in 16-byte pieces, all within its lines?
 bool in_pieces(const Operand &o, int64_t depth) {
@@ -526,24 +657,23 @@ uint64_t lines_bytes(const Operand &o, int64_t depth) {
 
 Choice choose(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t depth) {
   Choice c{Way::kSimple, 0, 1, false, false, 0, 0, 0, 0};
-  if (depth == 0 || m * n * depth < (1 << 18)) return c;
   // lines of 16-bit values are at most 2^22 bytes apart, so that a stage's offsets have 31 bits
   const auto too_long = [&](const Operand &o) { return (o.k_last ? depth : o.extent) > (1 << 21); };
-  if (too_long(a) || too_long(b)) return c;
+  if (depth == 0) return c;
+  if (m <= kFewRows && a.k_last && b.k_last && !a.scale && !b.scale) {
+    c.way = Way::kFew;
+    return c;
+  }
+  if (m * n * depth < (1 << 18) || too_long(a) || too_long(b)) return c;
   c.way = Way::kTile;
   c.lines_a = !in_pieces(a, depth), c.lines_b = !in_pieces(b, depth);
-  double best = 1e300;
   const int64_t steps = (depth + kStep - 1) / kStep;
-  for (int i = 0; i < 5; ++i) {
-    const TileSize &s = kTiles[i];
-    const int64_t tiles = ((m + s.m - 1) / s.m) * ((n + s.n - 1) / s.n), room = 256 * s.at_once;
-    for (int64_t splits = 1; splits <= 16 && splits * 8 <= steps + 7; ++splits) {
-      const int64_t rounds = (tiles * splits + room - 1) / room;
-      double cost = (double)rounds * s.m * s.n * s.at_once * ((steps + splits - 1) / splits + 8);
-      if (splits > 1) cost += (double)m * n * splits * 1.0;
-      if (cost < best) best = cost, c.tile = i, c.splits = (uint32_t)splits;
+  double best = 1e300;
+  for (int i = 0; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i)
+    for (int64_t splits = 1; splits <= 16 && splits * 4 <= steps + 3; ++splits) {
+      const double time = tile_time(kTiles[i], m, n, steps, splits);
+      if (time < best) best = time, c.tile = i, c.splits = (uint32_t)splits;
     }
-  }
   if (c.lines_a) c.at_a = c.bytes, c.bytes += lines_bytes(a, depth);
   if (c.lines_b) c.at_b = c.bytes, c.bytes += lines_bytes(b, depth);
   if (c.splits > 1) c.at_partial = c.bytes, c.bytes += (uint64_t)c.splits * m * n * 4;
@@ -599,6 +729,11 @@ int launch_product(const Operand &a, const Operand &b, const Epilogue &e, int64_
     DS_HIP_TRY(hipGetLastError());
     return DS_OK;
   }
+  if (c.way == Way::kFew) {
+    hipLaunchKernelGGL(ds_matmul_few_kernel<T>, dim3((uint32_t)((e.n + kFewCols - 1) / kFewCols)), dim3(kFewWaves * 64), 0, stream, a, b, e, depth);
+    DS_HIP_TRY(hipGetLastError());
+    return DS_OK;
+  }
   const TileSize &s = kTiles[c.tile];
   TileArgs t{{(const uint8_t *)a.base, a.ld * 2, a.extent}, {(const uint8_t *)b.base, b.ld * 2, b.extent}, depth,
              (uint32_t)((e.m + s.m - 1) / s.m), (uint32_t)((e.n + s.n - 1) / s.n), c.splits, c.splits > 1 ? (float *)(ws + c.at_partial) : nullptr};
@@ -608,8 +743,9 @@ int launch_product(const Operand &a, const Operand &b, const Epilogue &e, int64_
     case 0: DS_TRY((launch_tile<T, 8, 4, 2, 4, 2>(a, b, t, e, stream))); break;
     case 1: DS_TRY((launch_tile<T, 6, 4, 2, 4, 2>(a, b, t, e, stream))); break;
     case 2: DS_TRY((launch_tile<T, 4, 4, 2, 4, 3>(a, b, t, e, stream))); break;
-    case 3: DS_TRY((launch_tile<T, 4, 4, 2, 2, 2>(a, b, t, e, stream))); break;
-    default: DS_TRY((launch_tile<T, 1, 4, 4, 1, 5>(a, b, t, e, stream))); break;
+    case 3: DS_TRY((launch_tile<T, 2, 4, 4, 2, 3>(a, b, t, e, stream))); break;
+    case 4: DS_TRY((launch_tile<T, 2, 4, 2, 2, 3>(a, b, t, e, stream))); break;
+    default: DS_TRY((launch_tile<T, 1, 4, 4, 1, 3>(a, b, t, e, stream))); break;
   }
   if (c.splits == 1) return DS_OK;
   return launch_join(t.partial, t.splits, e, stream);
