@@ -478,11 +478,11 @@ __global__ __launch_bounds__(kThreads) void ds_matmul_lines_kernel(Operand o, in
 
 // ---- few rows of a, and a weight [out, in] -------------------------------------------------------------------------
 
-// At most 16 rows: what counts is reading b once, at the rate of HBM.  A work-group of eight wavefronts has 32 columns of c; a wavefront
+// At most 16 rows: what counts is reading b once, at the rate of HBM.  A work-group of eight wavefronts has 16 or 32 columns of c; a wavefront
 // takes every eighth piece of 64 k, so that neighbouring wavefronts read neighbouring lines, and asks for the next four pieces
 // before it multiplies these.  A lane reads 32 neighbouring bytes of a line of b, two matrix instructions' operands: the order of k within
 // a piece is any, as long as a's is the same.  The wavefronts' sums are added in their order, in LDS.
-constexpr int kFewRows = 16, kFewCols = 32, kFewWaves = 8;
+constexpr int kFewRows = 16, kFewWaves = 8;
 
 // Eight neighbouring k of line p from k on; what is beyond the matrix is 0.
 __device__ inline u32x4 line8(const Operand &o, int64_t p, int64_t k, int64_t depth) {
@@ -496,21 +496,21 @@ __device__ inline u32x4 line8(const Operand &o, int64_t p, int64_t k, int64_t de
   return r;
 }
 
-template <typename T>
+template <typename T, int SETS>
 __global__ __launch_bounds__(kFewWaves * 64) void ds_matmul_few_kernel(Operand a, Operand b, Epilogue e, int64_t depth) {
-  constexpr int kPieces = 4;
+  constexpr int kPieces = 4, kFewCols = SETS * 16;
   __shared__ float sums[kFewWaves][kFewRows][kFewCols + 4];
   __shared__ float out[kFewRows][kFewCols + 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, line = lane % 16;
   const int64_t q0 = (int64_t)blockIdx.x * kFewCols;
-  f32x4 sum[2] = {};
+  f32x4 sum[SETS] = {};
   struct Piece {
-    u32x4 w[2][2], x[2];
+    u32x4 w[SETS][2], x[2];
   };
   // lines beyond the matrix read its last one, and lead to sums that nobody stores
-  const uint16_t *from_w[2], *from_x;
+  const uint16_t *from_w[SETS], *from_x;
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
+  for (int s = 0; s < SETS; ++s) {
     const int64_t p = q0 + s * 16 + line;
     from_w[s] = (const uint16_t *)b.base + (p < b.extent ? p : b.extent - 1) * b.ld + lane / 16 * 16;
   }
@@ -519,7 +519,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void ds_matmul_few_kernel(Operand a
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) p.w[s][h] = *(const ds_u32x4 *)(from_w[s] + k + h * 8);
+      for (int s = 0; s < SETS; ++s) p.w[s][h] = *(const ds_u32x4 *)(from_w[s] + k + h * 8);
       p.x[h] = *(const ds_u32x4 *)(from_x + k + h * 8);
     }
   };
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void ds_matmul_few_kernel(Operand a
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) sum[s] = mfma(p.w[s][h], p.x[h], sum[s], T());
+      for (int s = 0; s < SETS; ++s) sum[s] = mfma(p.w[s][h], p.x[h], sum[s], T());
   };
   constexpr int64_t kApart = kFewWaves * 64;
   // this wavefront's whole pieces, the first `fours` of them four at a time
@@ -559,14 +559,14 @@ __global__ __launch_bounds__(kFewWaves * 64) void ds_matmul_few_kernel(Operand a
     for (int h = 0; h < 2; ++h) {
       const int64_t at = whole * 64 + lane / 16 * 16 + h * 8;
 #pragma unroll
-      for (int s = 0; s < 2; ++s) p.w[s][h] = line8(b, q0 + s * 16 + line, at, depth);
+      for (int s = 0; s < SETS; ++s) p.w[s][h] = line8(b, q0 + s * 16 + line, at, depth);
       p.x[h] = line8(a, line, at, depth);
     }
     multiply(p);
   }
   // a lane's sums: row lane % 16, columns 16 s + 4 (lane / 16) and on
 #pragma unroll
-  for (int s = 0; s < 2; ++s) *(f32x4 *)&sums[wave][line][s * 16 + lane / 16 * 4] = sum[s];
+  for (int s = 0; s < SETS; ++s) *(f32x4 *)&sums[wave][line][s * 16 + lane / 16 * 4] = sum[s];
   __syncthreads();
   if (threadIdx.x < kFewRows * kFewCols) {
     const int i = threadIdx.x / kFewCols, j = threadIdx.x % kFewCols;
@@ -579,11 +579,12 @@ __global__ __launch_bounds__(kFewWaves * 64) void ds_matmul_few_kernel(Operand a
   if (wave != 0) return;
   with_c_type(e, [&](auto type) {
     typedef decltype(type) C;
-    const int64_t i = lane / 4, j = q0 + lane % 4 * 8;
-    const int n = columns_of(e, i, j);
-    Eight z;
+    const int64_t i = lane / (SETS * 2), j = q0 + lane % (SETS * 2) * 8;
+    const int n = i < kFewRows ? columns_of(e, i, j) : 0;
+    Eight z = {};
+    if (n > 0)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) z.v[k] = out[i][lane % 4 * 8 + k];
+      for (int k = 0; k < 8; ++k) z.v[k] = out[i][lane % (SETS * 2) * 8 + k];
     finish8<C>(e, i, j, n, z, bias8(e, j, n), residual8<C>(e, i, j, n));
   });
 }
@@ -730,7 +731,11 @@ int launch_product(const Operand &a, const Operand &b, const Epilogue &e, int64_
     return DS_OK;
   }
   if (c.way == Way::kFew) {
-    hipLaunchKernelGGL(ds_matmul_few_kernel<T>, dim3((uint32_t)((e.n + kFewCols - 1) / kFewCols)), dim3(kFewWaves * 64), 0, stream, a, b, e, depth);
+    // 16 columns a work-group while those of 32 would leave CUs without one; a checkpoint's groups are 32
+    if (e.n <= 32 * kCus && !e.saved.base)
+      hipLaunchKernelGGL((ds_matmul_few_kernel<T, 1>), dim3((uint32_t)((e.n + 15) / 16)), dim3(kFewWaves * 64), 0, stream, a, b, e, depth);
+    else
+      hipLaunchKernelGGL((ds_matmul_few_kernel<T, 2>), dim3((uint32_t)((e.n + 31) / 32)), dim3(kFewWaves * 64), 0, stream, a, b, e, depth);
     DS_HIP_TRY(hipGetLastError());
     return DS_OK;
   }
