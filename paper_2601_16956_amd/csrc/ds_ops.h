@@ -201,19 +201,26 @@ __device__ inline uint32_t max_of_four_lanes(uint32_t m) {
 __device__ inline uint32_t mx8_scale(uint32_t top) {
   return top == 0 ? 0u : top >= 0x7f800000u ? 255u : (top >> 23) > 1u ? top >> 23 : 1u;
 }
-// Eight codes under that scale, as bytes.  x * 2^(133 - scale) is a power of two away from x, so exact, and at most 128
-// steps: the rounding to whole numbers is the only one.
+// Eight codes under that scale, as bytes.  x * 2^(133 - scale) is at most 128 steps; added to 1.5 * 2^23 in one operation, whose
+// rounding, to even, is the only one, it leaves the whole number of steps in the low bits.
 __device__ inline ds_u32x2 mx8_codes(const Eight &e, uint32_t scale) {
-  const int up = 133 - (int)scale;
-  uint32_t w[2] = {0, 0};
+  constexpr float kWhole = 12582912.f;
+  uint32_t q[8];
+  if (scale < 6u) {  // the factor is no float: magnitudes below 2^-121
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float q = __builtin_amdgcn_fmed3f(__builtin_rintf(ldexpf(e.v[k], up)), -127.f, 127.f);
-    w[k / 4] |= ((uint32_t)(int)q & 0xffu) << (8 * (k % 4));
+    for (int k = 0; k < 8; ++k) q[k] = (uint32_t)(int)__builtin_amdgcn_fmed3f(__builtin_rintf(ldexpf(e.v[k], 133 - (int)scale)), -127.f, 127.f);
+  } else {
+    const float steps = __uint_as_float((260u - (scale == 255u ? 133u : scale)) << 23);  // 2^(133 - scale)
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      q[k] = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fmaf(e.v[k], steps, kWhole), kWhole - 127.f, kWhole + 127.f));
   }
-  if (scale == 255u) w[0] = w[1] = 0;
   ds_u32x2 r;
-  r[0] = w[0], r[1] = w[1];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {  // the low bytes of four words: two, two, then all
+    const uint32_t low = __builtin_amdgcn_perm(q[4 * h + 1], q[4 * h], 0x0c0c0400u), high = __builtin_amdgcn_perm(q[4 * h + 3], q[4 * h + 2], 0x04000c0cu);
+    r[h] = scale == 255u ? 0u : low | high;
+  }
   return r;
 }
 // The step of a group, 2^(scale - 133); NaN where the group has no values.
