@@ -15,11 +15,12 @@ namespace {
 constexpr int kThreads = 256;
 
 // Work items are pieces of eight columns; a row has a multiple of four of them, so that a group's are four neighbouring lanes.
-// (A division in 64 bits takes as long as the rest.  Index: uint32_t where it holds their number.)
+// (A division in 64 bits takes as long as the rest.  Index: uint32_t where it holds their number; `shift` is the binary logarithm of
+// `pieces`, or -1 where that is none.)
 template <typename T, typename Index>
-__global__ __launch_bounds__(kThreads) void ds_mx8_save_kernel(Rows x, Rows saved, int64_t rows, int64_t cols, uint32_t pieces) {
+__global__ __launch_bounds__(kThreads) void ds_mx8_save_kernel(Rows x, Rows saved, int64_t rows, int64_t cols, uint32_t pieces, int shift) {
   for (int64_t first = (int64_t)blockIdx.x * kThreads; first < rows * pieces; first += (int64_t)gridDim.x * kThreads) {
-    const Index item = (Index)(first + threadIdx.x), row = item / (Index)pieces;
+    const Index item = (Index)(first + threadIdx.x), row = shift >= 0 ? item >> shift : item / (Index)pieces;
     const int64_t i = row, j = (int64_t)(item - row * (Index)pieces) * 8, left = i < rows ? cols - j : 0;
     const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
     mx8_put(saved, i, j, n, RowsOf<T>::get(x, i, j, n));
@@ -27,9 +28,9 @@ __global__ __launch_bounds__(kThreads) void ds_mx8_save_kernel(Rows x, Rows save
 }
 
 template <typename T, typename Index>
-__global__ __launch_bounds__(kThreads) void ds_mx8_load_kernel(Rows saved, Rows x, int64_t rows, int64_t cols, uint32_t pieces) {
+__global__ __launch_bounds__(kThreads) void ds_mx8_load_kernel(Rows saved, Rows x, int64_t rows, int64_t cols, uint32_t pieces, int shift) {
   for (int64_t first = (int64_t)blockIdx.x * kThreads; first < rows * pieces; first += (int64_t)gridDim.x * kThreads) {
-    const Index item = (Index)(first + threadIdx.x), row = item / (Index)pieces;
+    const Index item = (Index)(first + threadIdx.x), row = shift >= 0 ? item >> shift : item / (Index)pieces;
     const int64_t i = row, j = (int64_t)(item - row * (Index)pieces) * 8, left = i < rows ? cols - j : 0;
     const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
     put_up_to8<T>(x.base, i * x.stride + j, n, RowsOf<Mx8>::get(saved, i, j, n));
@@ -48,11 +49,12 @@ int launch_mx8(const ds_matrix *x, const ds_matrix *saved, hipStream_t stream) {
   if (x->rows == 0 || x->cols == 0) return DS_OK;
   const int64_t pieces = ds_groups(x->cols) * (kGroup / 8), all = (x->rows * pieces + kThreads - 1) / kThreads;
   const int64_t grid = all < kMaxGrid ? all : kMaxGrid;
+  const int shift = (pieces & (pieces - 1)) == 0 ? __builtin_ctzll(pieces) : -1;
   const bool narrow = all <= (int64_t)0xffffffff / kThreads;
   return ds_with_type(x->dtype, [&](auto type) -> int {
     typedef decltype(type) T;
     const auto launch = [&](auto kernel, const ds_matrix *from, const ds_matrix *to) -> int {
-      hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(kThreads), 0, stream, ds_rows(from), ds_rows(to), x->rows, x->cols, (uint32_t)pieces);
+      hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(kThreads), 0, stream, ds_rows(from), ds_rows(to), x->rows, x->cols, (uint32_t)pieces, shift);
       DS_HIP_TRY(hipGetLastError());
       return DS_OK;
     };

@@ -65,18 +65,20 @@ __global__ __launch_bounds__(WIDE * 64) void ds_layernorm_forward_kernel(NormFor
   const int at = threadIdx.x % (WAVES * 64) * 8, which = threadIdx.x / (WAVES * 64);
   Eight g[HAS], b[HAS];
   int n[HAS];
-#pragma unroll
-  for (int p = 0; p < HAS; ++p) {
-    const int64_t j = at + p * kApart;
-    n[p] = columns_left(a.cols, j);
-    g[p] = get_up_to8_any(a.gamma, a.param_dtype, j, n[p], 1.f), b[p] = get_up_to8_any(a.beta, a.param_dtype, j, n[p], 0.f);
-  }
   const float each = 1.f / (float)a.cols;
   const int64_t stride = (int64_t)gridDim.x * kRows;
   int64_t i = (int64_t)blockIdx.x * kRows + which;
   typename RowsOf<T>::Bits next[HAS];
+  AnyBits gamma[HAS], beta[HAS];
 #pragma unroll
-  for (int p = 0; p < HAS; ++p) next[p] = RowsOf<T>::ask(a.x, i, at + p * kApart, i < a.rows ? n[p] : 0);
+  for (int p = 0; p < HAS; ++p) {
+    const int64_t j = at + p * kApart;
+    n[p] = columns_left(a.cols, j);
+    next[p] = RowsOf<T>::ask(a.x, i, j, i < a.rows ? n[p] : 0);
+    gamma[p] = ask_up_to8_any(a.gamma, a.param_dtype, j, n[p]), beta[p] = ask_up_to8_any(a.beta, a.param_dtype, j, n[p]);
+  }
+#pragma unroll
+  for (int p = 0; p < HAS; ++p) g[p] = value_any(gamma[p], a.gamma, a.param_dtype, 1.f), b[p] = value_any(beta[p], a.beta, a.param_dtype, 0.f);
   for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.rows; first += stride, i += stride) {
     Eight x[HAS];
     float sum = 0.f, squares = 0.f;
@@ -164,10 +166,11 @@ __global__ __launch_bounds__(WIDE * 64) void ds_layernorm_backward_kernel(NormBa
   const int at = threadIdx.x % (WAVES * 64) * 8, which = threadIdx.x / (WAVES * 64);
   Eight g[HAS], dg[HAS] = {}, db[HAS] = {};
   int n[HAS];
+  AnyBits gamma[HAS];
 #pragma unroll
   for (int p = 0; p < HAS; ++p) {
     n[p] = columns_left(a.cols, at + p * kApart);
-    g[p] = get_up_to8_any(a.gamma, a.param_dtype, at + p * kApart, n[p], 1.f);
+    gamma[p] = ask_up_to8_any(a.gamma, a.param_dtype, at + p * kApart, n[p]);
   }
   const float each = 1.f / (float)a.cols;
   const int64_t stride = (int64_t)gridDim.x * kRows;
@@ -190,6 +193,8 @@ __global__ __launch_bounds__(WIDE * 64) void ds_layernorm_backward_kernel(NormBa
   };
   Row next = {};
   ask(next, i);
+#pragma unroll
+  for (int p = 0; p < HAS; ++p) g[p] = value_any(gamma[p], a.gamma, a.param_dtype, 1.f);
   int turn = 0;
   for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.rows; first += stride, i += stride, turn ^= 1) {
     Row now = next;

@@ -138,10 +138,7 @@ struct Elem<__half> {
   }
 };
 
-// Element i of a vector whose type is known at run time only (a bias, gamma: few of them, read once a row or tile).
-__device__ inline float get_any(const void *p, uint32_t dtype, int64_t i) {
-  return dtype == DS_F32 ? ((const float *)p)[i] : dtype == DS_BF16 ? Elem<__hip_bfloat16>::get(p, i) : Elem<__half>::get(p, i);
-}
+// Eight elements of a vector whose type is known at run time only (a bias, gamma: few of them, read once a row or tile).
 __device__ inline Eight get8_any(const void *p, uint32_t dtype, int64_t i) {
   return dtype == DS_F32 ? Elem<float>::get8(p, i) : dtype == DS_BF16 ? Elem<__hip_bfloat16>::get8(p, i) : Elem<__half>::get8(p, i);
 }
@@ -162,18 +159,42 @@ __device__ inline void put_up_to8(void *p, int64_t i, int n, const Eight &e) {
   for (int k = 0; k < 8; ++k)
     if (k < n) Elem<T>::put(p, i + k, e.v[k]);
 }
-__device__ inline Eight get_up_to8_any(const void *p, uint32_t dtype, int64_t i, int n, float without) {
+// In two halves: the bits of several such vectors are on their way together, where making floats of one would wait for it.
+struct AnyBits {
+  ds_u32x4 w[2];
+};
+__device__ inline AnyBits ask_up_to8_any(const void *p, uint32_t dtype, int64_t i, int n) {
+  AnyBits b = {};
+  if (!p || n <= 0) return b;
+  if (dtype == DS_F32) {
+    const uint32_t *q = (const uint32_t *)p + i;
+    if (n >= 8) b.w[0] = *(const ds_u32x4 *)q, b.w[1] = *(const ds_u32x4 *)(q + 4);
+    else
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < n) b.w[k / 4][k % 4] = q[k];
+  } else {
+    const uint16_t *q = (const uint16_t *)p + i;
+    if (n >= 8) b.w[0] = *(const ds_u32x4 *)q;
+    else
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < n) b.w[0][k / 2] |= (uint32_t)q[k] << (16 * (k % 2));
+  }
+  return b;
+}
+// `without`: what stands for a vector that there is none of.
+__device__ inline Eight value_any(const AnyBits &b, const void *p, uint32_t dtype, float without) {
   Eight e;
   if (!p) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) e.v[k] = without;
-  } else if (n >= 8) {
-    e = get8_any(p, dtype, i);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) e.v[k] = k < n ? get_any(p, dtype, i + k) : 0.f;
+    return e;
   }
-  return e;
+  return get8_any(&b, dtype, 0);
+}
+__device__ inline Eight get_up_to8_any(const void *p, uint32_t dtype, int64_t i, int n, float without) {
+  return value_any(ask_up_to8_any(p, dtype, i, n), p, dtype, without);
 }
 
 // ---- device: checkpoints in 8 bits -----------------------------------------------------------------------------
