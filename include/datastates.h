@@ -732,8 +732,8 @@ int ds_matmul(const ds_matrix *a, const ds_matrix *b, const ds_matrix *c, const 
 /*
  * The gradient of c = act(z) with z = product + bias:
  *   dz = dy * act'(z),  dbias_j = sum over rows of dz (before dz is rounded).
- * dy, dz: DS_F32, DS_BF16 or DS_F16, the same for both, ROWS; dz may be dy itself.  z: that
- * type, or a DS_MX8 checkpoint.  dbias: NULL, or cols floats, overwritten (with
+ * dy, dz: DS_F32, DS_BF16 or DS_F16, the same for both, ROWS.  z: that type, or a
+ * DS_MX8 checkpoint.  dz may be dy itself, or z.  dbias: NULL, or cols floats, overwritten (with
  * zeros where there are no rows).  Errors: DS_EINVAL, DS_ERANGE, DS_EHIP.
  */
 int ds_activation_backward_workspace(int64_t rows, int64_t cols, uint64_t *bytes);

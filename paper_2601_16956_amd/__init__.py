@@ -719,12 +719,13 @@ def ds_image_compress(image_dev: int, nbytes: int, block_bytes: int, keep_dev: i
 
 # ---- the training step between two snapshots ----------------------------------
 
-_float_codes = None
+_float_codes: dict = {}
+_byte_types: tuple = ()
 
 
 def _float_code(dtype) -> int:
     global _float_codes
-    if _float_codes is None:
+    if not _float_codes:
         import torch
         _float_codes = {torch.float32: DS_F32, torch.bfloat16: DS_BF16, torch.float16: DS_F16}
     code = _float_codes.get(dtype)
@@ -748,19 +749,22 @@ def make_matrix(tensor) -> ds_matrix:
 def make_mx8(codes, scale) -> ds_matrix:
     """A checkpoint in 8 bits out of two torch tensors on the GPU: int8 codes [rows, cols] and uint8 scales
     [rows, ceil(cols / 32)], both with neighbouring columns next to each other."""
-    import torch
-    if codes.dtype != torch.int8 or scale.dtype != torch.uint8:
+    global _byte_types
+    if not _byte_types:
+        import torch
+        _byte_types = (torch.int8, torch.uint8)
+    if codes.dtype is not _byte_types[0] or scale.dtype is not _byte_types[1]:
         raise TypeError("codes are int8, scales uint8")
     if not (codes.is_cuda and scale.is_cuda):
         raise ValueError("codes and scales are in device memory")
     if codes.dim() != 2 or scale.dim() != 2:
         raise ValueError("codes and scales have two dimensions")
-    rows, cols = codes.shape
-    if tuple(scale.shape) != (rows, -(-cols // 32)):
-        raise ValueError(f"codes of {rows} x {cols} have scales of {rows} x {-(-cols // 32)}, not {tuple(scale.shape)}")
-    if scale.shape[1] > 1 and scale.stride(1) != 1:
+    (rows, cols), (lines, groups), (down, across) = codes.shape, scale.shape, scale.stride()
+    if lines != rows or groups != -(-cols // 32):
+        raise ValueError(f"codes of {rows} x {cols} have scales of {rows} x {-(-cols // 32)}, not {lines} x {groups}")
+    if groups > 1 and across != 1:
         raise ValueError("the scales of a row are not next to each other")
-    return ds_matrix(codes.data_ptr(), DS_MX8, 0, rows, cols, codes.stride(0), codes.stride(1), scale.data_ptr(), scale.stride(0))
+    return ds_matrix(codes.data_ptr(), DS_MX8, 0, rows, cols, *codes.stride(), scale.data_ptr(), down)
 
 
 def make_epilogue(bias=None, act: int = DS_ACT_NONE, residual: Optional[ds_matrix] = None,
@@ -782,11 +786,6 @@ def make_epilogue(bias=None, act: int = DS_ACT_NONE, residual: Optional[ds_matri
     return ep
 
 
-def _workspace_bytes(rc: int, out, where: str) -> int:
-    _check(rc, where)
-    return out.value
-
-
 def ds_mx8_save(x: ds_matrix, saved: ds_matrix, stream: int = 0) -> None:
     _check(_lib.ds_mx8_save(x, saved, stream), "ds_mx8_save")
 
@@ -803,7 +802,8 @@ def ds_layernorm_forward(x: ds_matrix, gamma: Optional[int], beta: Optional[int]
 
 def ds_layernorm_backward_workspace(rows: int, cols: int) -> int:
     out = ctypes.c_uint64(0)
-    return _workspace_bytes(_lib.ds_layernorm_backward_workspace(rows, cols, out), out, "ds_layernorm_backward_workspace")
+    _check(_lib.ds_layernorm_backward_workspace(rows, cols, out), "ds_layernorm_backward_workspace")
+    return out.value
 
 
 def ds_layernorm_backward(dy: ds_matrix, x: ds_matrix, mean: int, rstd: int, gamma: Optional[int], param_dtype: int,
@@ -815,7 +815,8 @@ def ds_layernorm_backward(dy: ds_matrix, x: ds_matrix, mean: int, rstd: int, gam
 
 def ds_matmul_workspace(a: ds_matrix, b: ds_matrix, c: ds_matrix) -> int:
     out = ctypes.c_uint64(0)
-    return _workspace_bytes(_lib.ds_matmul_workspace(a, b, c, out), out, "ds_matmul_workspace")
+    _check(_lib.ds_matmul_workspace(a, b, c, out), "ds_matmul_workspace")
+    return out.value
 
 
 def ds_matmul(a: ds_matrix, b: ds_matrix, c: ds_matrix, epilogue: Optional[ds_matmul_epilogue] = None,
@@ -825,7 +826,8 @@ def ds_matmul(a: ds_matrix, b: ds_matrix, c: ds_matrix, epilogue: Optional[ds_ma
 
 def ds_activation_backward_workspace(rows: int, cols: int) -> int:
     out = ctypes.c_uint64(0)
-    return _workspace_bytes(_lib.ds_activation_backward_workspace(rows, cols, out), out, "ds_activation_backward_workspace")
+    _check(_lib.ds_activation_backward_workspace(rows, cols, out), "ds_activation_backward_workspace")
+    return out.value
 
 
 def ds_activation_backward(dy: ds_matrix, z: ds_matrix, act: int, dz: ds_matrix, dbias: Optional[int],

@@ -349,7 +349,8 @@ def test_the_norm_s_gradient_is_the_forward_pass_s_differences():
 def test_activation_backward(rows, cols, kind, act):
     rng = np.random.default_rng(rows * 31 + cols)
     for case, (pad, shift) in enumerate(((0, 0), (3, 1), (8, 8))):
-        z, dy = Mat(3 * rng.standard_normal((rows, cols)), kind, pad, shift), Mat(rng.standard_normal((rows, cols)), kind, pad, shift)
+        dy0 = rng.standard_normal((rows, cols))
+        z, dy = Mat(3 * rng.standard_normal((rows, cols)), kind, pad, shift), Mat(dy0, kind, pad, shift)
         dz = Mat(np.zeros((rows, cols)), kind, pad, shift)
         read, m = z.np(), z.m
         if case != 1:
@@ -371,6 +372,12 @@ def test_activation_backward(rows, cols, kind, act):
         first = dz.np()
         ds.ds_activation_backward(dy.m, m, ACT[act], dy.m, None, None, 0, stream())
         assert np.array_equal(dy.np(), first) and dy.rest_untouched()
+        if case == 1:  # and over z
+            again = Mat(want, kind, pad, shift)
+            again.t.copy_(torch.from_numpy(np.ascontiguousarray(z.np(), dtype=np.float32)))
+            dy2 = Mat(dy0, kind, pad, shift)
+            ds.ds_activation_backward(dy2.m, again.m, ACT[act], again.m, None, None, 0, stream())
+            assert np.array_equal(again.np(), first) and again.rest_untouched()
 
 
 def test_activation_backward_of_no_rows_and_of_far_values():
