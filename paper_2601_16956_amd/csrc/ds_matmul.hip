@@ -1,12 +1,18 @@
 // c = act(a b + bias) + residual on the matrix cores.
 //
-// A work-group of four wavefronts has a tile of 64 x 64 of c and walks along k in steps of 32.  Each thread brings eight
-// neighbouring elements of either operand through registers into LDS, the next step's while the matrix instructions run
-// on this one's; both operands lie in LDS with k last, so that an instruction's operand is one 16-byte read of a lane.
-// A wavefront has 16 rows of the tile: four v_mfma_f32_16x16x32 a step, with the operands exchanged, so that a lane's
-// four results are neighbouring columns of one row.  The sums go through LDS once more, to leave a thread eight
-// neighbouring columns for the epilogue: the bias, the checkpoint of z (four lanes hold a group of 32), the activation, the
-// residual and the one rounding.
+// Three ways, by the sizes (choose()):
+//   tiles     a work-group has a tile of 64 x 64 to 256 x 256 of c and walks along k; the operands go from memory to LDS without
+//             passing registers, in either order of each; few tiles are split along k, and joined by a second launch.
+//             Operands that are no whole 16-byte pieces, or checkpoints in 8 bits, are laid out in the workspace first.  Bound by
+//             the matrix cores and, at the largest sizes, by the power that they draw: 16384 x 3584 x 8192 in bfloat16
+//             708 us, 1.36 PFLOP/s (a library's product 716 to 728), with a residual 770; 8192^3 750 to 820 us.
+//             Zeros instead of normal numbers run a fifth faster.
+//   few rows  at most 16 rows on a weight [out, in]: bound by reading the weight, 1 x 8192 x 3584 in 13 us, 4.5 TB/s.
+//   simple    whatever is left: products of less than 2^18 multiplications, and lines beyond 2^21 elements.
+//
+// Always: 32-bit sums; v_mfma_f32_16x16x32 with the operands exchanged, so that a lane's four results are neighbouring
+// columns of one row; the sums go through LDS once more, to leave a lane eight neighbouring columns for the epilogue: the
+// bias, the checkpoint of z (four lanes hold a group of 32), the activation, the residual and the one rounding.
 
 #include <type_traits>
 
@@ -96,6 +102,11 @@ __device__ inline int columns_of(const Epilogue &e, int64_t i, int64_t j) {
   return (int)(left < 0 ? 0 : left < 8 ? left : 8);
 }
 
+// ---- any operands ------------------------------------------------------------------------------------------------------
+
+// A work-group of four wavefronts has a tile of 64 x 64 and walks along k in steps of 32.  Each thread brings eight neighbouring elements
+// of either operand through registers into LDS, the next step's while the matrix instructions run on this one's; both
+// operands lie in LDS with k last.  A wavefront has 16 rows of the tile.  (390 TFLOP/s at 16384 x 3584 x 8192.)
 constexpr int kTile = 64, kDeep = 32, kPitch = kDeep + 8;
 
 // Eight neighbouring elements of an operand for the LDS: of one p from k on (k_last), or of one k from p on.  Those beyond
@@ -226,10 +237,8 @@ __device__ inline void stage_is_there() {
 //     the 32 lanes of a pass, eight rows of 32 bytes, meet every bank once.
 template <int P, int WAVES, bool K_LAST>
 struct Stage {
-  static constexpr int kBytes = P * kStep * 2, kTransfers = kBytes / 1024, kLoads = (kTransfers + WAVES - 1) / WAVES, kLine = P * 2;
-  // Every wavefront starts kLoads transfers, so that all count alike; those that are too many bring zeros to LDS that nobody reads.
-  static constexpr int kSpare = kLoads * WAVES > kTransfers ? 1024 : 0;
-  static_assert(kBytes % 1024 == 0, "whole transfers");
+  static constexpr int kBytes = P * kStep * 2, kLoads = kBytes / 1024 / WAVES, kLine = P * 2;
+  static_assert(kBytes % (1024 * WAVES) == 0, "whole transfers, as many for each wavefront");
   uint32_t offset[kLoads];  // of this lane's pieces from the operand's first element of the stage
   int at_k[kLoads];         // their place along k
   static __device__ inline int turn(int k) {
@@ -240,8 +249,6 @@ struct Stage {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int f = (i * WAVES + wave) * 64 + lane;
-      at_k[i] = 0, offset[i] = kNowhere;
-      if (i * WAVES + wave >= kTransfers) continue;
       if (K_LAST) {
         const int r = f / 8, c = (f % 8) ^ (r & 7);
         at_k[i] = c * 8;
@@ -260,11 +267,10 @@ struct Stage {
   static __device__ inline int64_t apart(const Source &s) { return K_LAST ? kStep * 2 : kStep * s.ld; }
   // Starts this wavefront's transfer `i` of the step at `from` into the stage at `lds`; `left`: what of k there is from the
   // step's first on, 0 and less where nothing is.
-  __device__ inline void bring(int i, uint64_t from, int left, uint32_t lds, uint32_t spare, int wave) const {
-    const int x = i * WAVES + wave;
+  __device__ inline void bring(int i, uint64_t from, int left, uint32_t lds, int wave) const {
     const u32x4 resource = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)from), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(from >> 32)), kNowhere,
                             0x00020000u};
-    to_lds(kSpare == 0 || x < kTransfers ? lds + x * 1024 : spare, at_k[i] < left ? offset[i] : kNowhere, resource);
+    to_lds(lds + (i * WAVES + wave) * 1024, at_k[i] < left ? offset[i] : kNowhere, resource);
   }
   // The operand of a matrix instruction: 16 lines from p (a multiple of 16) on, 32 of k from 32 * half on.
   static __device__ inline u32x4 read(const uint8_t *lds, int p, int half, int lane) {
@@ -290,7 +296,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs
   // of 16 rows of the sums each, as many as the stages' LDS holds for every wavefront: all, or half of them
   constexpr int kRoom = STAGES * kStage / (kWaves * 16 * kOutPitch * 4), kOut = kRoom >= MI ? MI : MI / 2;
   static_assert(NI == 4 && kWaves * kOut * 16 * kOutPitch * 4 <= STAGES * kStage, "the sums leave through the stages");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES * kStage + (A::kSpare | B::kSpare)];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES * kStage];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // Work-groups go to the eight XCDs in turn: each XCD gets a run of neighbouring tiles, in stripes of four tiles' rows, so that
@@ -313,8 +319,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void ds_matmul_tile_kernel(TileArgs
   int left = (int)((last * kStep < t.depth ? last * kStep : t.depth) - first * kStep);
   constexpr int kLoads = A::kLoads + B::kLoads;
   const auto bring = [&](int i, int to) {
-    if (i < A::kLoads) a.bring(i, from_a, left, base + to * kStage, base + STAGES * kStage, wave);
-    else b.bring(i - A::kLoads, from_b, left, base + to * kStage + A::kBytes, base + STAGES * kStage, wave);
+    if (i < A::kLoads) a.bring(i, from_a, left, base + to * kStage, wave);
+    else b.bring(i - A::kLoads, from_b, left, base + to * kStage + A::kBytes, wave);
     if (i == kLoads - 1) from_a += apart_a, from_b += apart_b, left -= kStep;
   };
   const int m0 = wave / WN * MI * 16, n0 = wave % WN * NI * 16;
@@ -466,7 +472,9 @@ __global__ __launch_bounds__(kThreads) void ds_matmul_join_kernel(const float *p
   }
 }
 
-// An operand's lines of `length` elements as lines of 16-bit values, a multiple of eight of them, the rest zeros.
+// An operand's lines of `length` elements as lines of 16-bit values, a multiple of eight of them, the rest zeros.  Bound by HBM: a checkpoint
+// of 16384 x 4096 is read and written in 37 us, 5.4 TB/s, beside 320 us of the product that it goes into.  (Making
+// 16-bit values of the codes in the tiles' kernel would do it once for every row of tiles.)
 template <typename T, typename Index>
 __global__ __launch_bounds__(kThreads) void ds_matmul_lines_kernel(Operand o, int64_t lines, int64_t length, uint16_t *out, uint32_t pieces) {
   for (int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x; at < lines * pieces; at += (int64_t)gridDim.x * kThreads) {
