@@ -129,6 +129,58 @@ __global__ __launch_bounds__(kThreads) void ds_sum_parts_kernel(const float *par
   }
 }
 
+// Few rows: a work-group has 64 columns, eight lanes a row of them and 128 rows at a time, and sums the bias's gradient itself: one launch.
+// So / by the kernel above and the sum of its lines, us of the GPU, silu on bfloat16 from 8 bits: 1 x 1024 4.0 / 4.9, 64 x 16384 4.6 / 6.3,
+// 128 x 1024 4.6 / 5.3, 333 x 1024 5.8 / 5.8, 512 x 1024 7.2 / 5.7; a caller who does not wait in between, 333 x 1024, 10.8 /
+// 14.2.
+constexpr int64_t kFewRows = 384, kFewCols = 16384;
+template <typename T, typename Z, uint32_t ACT>
+__global__ __launch_bounds__(1024) void ds_activation_backward_few_kernel(Rows dy, Rows z, Rows dz, int rows, int64_t cols, float *dbias) {
+  __shared__ float sums[128][64 + 1];
+  const int across = threadIdx.x % 8, row = threadIdx.x / 8;
+  const int64_t j = (int64_t)blockIdx.x * 64 + across * 8, left = cols - j;
+  const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
+  constexpr int kTimes = (int)kFewRows / 128;
+  typename RowsOf<T>::Bits d[kTimes];
+  typename RowsOf<Z>::Bits at[kTimes];
+#pragma unroll
+  for (int u = 0; u < kTimes; ++u) {
+    const int i = u * 128 + row;
+    d[u] = RowsOf<T>::ask(dy, i, j, i < rows ? n : 0), at[u] = RowsOf<Z>::ask(z, i, j, i < rows ? n : 0);
+  }
+  Eight sum = {};
+#pragma unroll
+  for (int u = 0; u < kTimes; ++u) {
+    const int i = u * 128 + row;
+    if (i >= rows) break;
+    const Eight g = RowsOf<T>::value(d[u], n), x = RowsOf<Z>::value(at[u], n);
+    Eight r;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      r.v[k] = g.v[k] * activation_slope<ACT>(x.v[k]);
+      sum.v[k] += k < n ? r.v[k] : 0.f;
+    }
+    put_up_to8<T>(dz.base, i * dz.stride + j, n, r);
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sums[row][across * 8 + k] = sum.v[k];
+  // 128 sums of a column, 16 lanes eight of them each, then those 16 in their order
+  __syncthreads();
+  const int column = threadIdx.x / 16, part = threadIdx.x % 16;
+  float s = 0.f;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) s += sums[part * 8 + r][column];
+  __syncthreads();
+  sums[part][column] = s;
+  __syncthreads();
+  if (threadIdx.x < 64 && (int64_t)blockIdx.x * 64 + threadIdx.x < cols) {
+    float total = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) total += sums[r][threadIdx.x];
+    dbias[(int64_t)blockIdx.x * 64 + threadIdx.x] = total;
+  }
+}
+
 constexpr int64_t kActGroups = 2048;  // work-groups of a launch, about
 int64_t act_parts(int64_t rows, int64_t cols) {
   const int64_t across = cols > 512 ? (cols + 511) / 512 : 1, by_rows = (rows + 3) / 4, by_grid = (kActGroups + across - 1) / across;
@@ -175,13 +227,20 @@ extern "C" int ds_activation_backward(const ds_matrix *dy, const ds_matrix *z, u
     if (workspace_bytes < (uint64_t)(parts * cols * 4)) return DS_ERANGE;
   }
   hipStream_t st = (hipStream_t)stream;
+  const bool few = dbias && rows > 0 && rows <= kFewRows && cols <= kFewCols;
   if (rows > 0) {
     const dim3 grid((uint32_t)((cols + 511) / 512), (uint32_t)parts);
     const int rc = ds_with_type(dy->dtype, [&](auto type) -> int {
       typedef decltype(type) T;
       return ds_with_act(act, [&](auto a) -> int {
         constexpr uint32_t A = decltype(a)::value;
-        if (z->dtype == DS_MX8)
+        if (few) {
+          const auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((uint32_t)((cols + 63) / 64)), dim3(1024), 0, st, ds_rows(dy), ds_rows(z), ds_rows(dz), (int)rows, cols, dbias);
+          };
+          if (z->dtype == DS_MX8) launch(ds_activation_backward_few_kernel<T, Mx8, A>);
+          else launch(ds_activation_backward_few_kernel<T, T, A>);
+        } else if (z->dtype == DS_MX8)
           hipLaunchKernelGGL((ds_activation_backward_kernel<T, Mx8, A>), grid, dim3(kThreads), 0, st, ds_rows(dy), ds_rows(z),
                              ds_rows(dz), rows, cols, dbias ? (float *)workspace : nullptr);
         else
@@ -193,5 +252,5 @@ extern "C" int ds_activation_backward(const ds_matrix *dy, const ds_matrix *z, u
     });
     DS_TRY(rc);
   }
-  return dbias ? ds_launch_sum_parts((const float *)workspace, rows > 0 ? parts : 0, cols, dbias, nullptr, st) : DS_OK;
+  return dbias && !few ? ds_launch_sum_parts((const float *)workspace, rows > 0 ? parts : 0, cols, dbias, nullptr, st) : DS_OK;
 }
