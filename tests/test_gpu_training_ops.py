@@ -478,6 +478,37 @@ def test_matmul_of_long_sums(m, k, n):
         product_case(m, k, n, layout=layout, out="f32")
 
 
+@pytest.mark.parametrize("layout", ("nt", "nn", "tn", "tt"))
+@pytest.mark.parametrize("m,k,n", [(3904, 520, 3904), (3900, 515, 3901), (2752, 328, 4096), (2750, 333, 4090), (1984, 200, 3992), (1990, 203, 3990),
+                                   (1504, 600, 2000), (1500, 601, 2001), (704, 5000, 2104), (700, 5001, 2100), (1104, 496, 1304), (304, 16384, 304),
+                                   (600, 3000, 704)])
+def test_matmul_of_every_tile(m, k, n, layout):
+    """Sizes at which tiles of 256 x 256, 192 x 256, 128 x 256, 128 x 128, 64 x 128 and 64 x 64 are chosen, whole and split along k, with
+    operands in whole 16-byte pieces and not; against products in 64 bits on the GPU, within the bounds of product_case."""
+    g = torch.Generator(device="cuda").manual_seed(m + k + n)
+    for kind, out, act in (("bf16", "bf16", "gelu_tanh"), ("f16", "f32", "none")):
+        dtype, stored = TYPES[kind][0], lambda r, c, t: torch.randn(*((c, r) if t else (r, c)), generator=g, device="cuda").to(TYPES[kind][0])
+        a = stored(m, k, layout[0] == "t").t() if layout[0] == "t" else stored(m, k, False)
+        b = stored(k, n, layout[1] == "t").t() if layout[1] == "t" else stored(k, n, False)
+        bias, residual = torch.randn(n, generator=g, device="cuda").to(dtype), torch.randn(m, n, generator=g, device="cuda").to(TYPES[out][0])
+        c, q, s = torch.full((m, n + 8), 7.0, dtype=TYPES[out][0], device="cuda"), *_room8(m, n)
+        A, B, C = ds.make_matrix(a), ds.make_matrix(b), ds.make_matrix(c[:, :n])
+        need = ds.ds_matmul_workspace(A, B, C)
+        ws, whole = workspace(need)
+        ds.ds_matmul(A, B, C, ds.make_epilogue(bias=bias, act=ACT[act], residual=ds.make_matrix(residual), saved=ds.make_mx8(q, s)), ws.data_ptr(),
+                     need, stream())
+        a64, b64 = a.double().contiguous(), b.double().contiguous()
+        z = a64 @ b64 + bias.double()
+        dz = 2 * (k + 8) * E * (a64.abs() @ b64.abs() + bias.double().abs())
+        want = (z * torch.sigmoid(2 * (2 / np.pi) ** 0.5 * (z + 0.044715 * z ** 3)) if act != "none" else z) + residual.double()
+        dc = 1.13 * dz + (0 if act == "none" else 32 * E * z.abs() * (1 + z.abs())) + 2 * E * (want.abs() + residual.double().abs())
+        assert ((c[:, :n].double() - want).abs() <= dc + U[out] * (want.abs() + dc) + TINY[out]).all()
+        assert (c[:, n:] == 7).all() and whole()
+        step = (2.0 ** (s.double() - 133)).repeat_interleave(32, 1)[:, :n]
+        held = q.double() * step
+        assert ((held - z).abs() <= dz + torch.where(q.abs() == 127, step, step / 2)).all()
+
+
 def test_matmul_onto_itself():
     rng = np.random.default_rng(3)
     for m, n in ((1, 64), (200, 136), (128, 256)):
