@@ -67,8 +67,7 @@ class Block:
 
     def forward(self, x):
         M, p, stream = ds.make_matrix, self.param, torch.cuda.current_stream().cuda_stream
-        ds.ds_layernorm_forward(M(x), p["gamma"].data_ptr(), p["beta"].data_ptr(), ds.DS_BF16, EPS, M(self.normed),
-                                self.mean.data_ptr(), self.rstd.data_ptr(), self.x8.m, stream)
+        ds.ds_layernorm_forward(M(x), p["gamma"], p["beta"], ds.DS_BF16, EPS, M(self.normed), self.mean, self.rstd, self.x8.m, stream)
         ds.ds_mx8_save(M(self.normed), self.normed8.m, stream)
         self._matmul(M(self.normed), M(p["fc1.w"].t()), M(self.h),
                      ds.make_epilogue(bias=p["fc1.b"], act=ds.DS_ACT_GELU_TANH, saved=self.z8.m))
@@ -81,15 +80,15 @@ class Block:
         M, p, g, stream = ds.make_matrix, self.param, self.grad, torch.cuda.current_stream().cuda_stream
         self._matmul(M(dy.t()), self.h8.m, M(g["fc2.w"]))
         room = self._room(ds.ds_activation_backward_workspace(self.rows, self.hidden))
-        ds.ds_activation_backward(M(dy), M(dy), ds.DS_ACT_NONE, M(dy), g["fc2.b"].data_ptr(), *room, stream)
+        ds.ds_activation_backward(M(dy), M(dy), ds.DS_ACT_NONE, M(dy), g["fc2.b"], *room, stream)
         self._matmul(M(dy), M(p["fc2.w"]), M(self.dh))
         room = self._room(ds.ds_activation_backward_workspace(self.rows, self.ffn))
-        ds.ds_activation_backward(M(self.dh), self.z8.m, ds.DS_ACT_GELU_TANH, M(self.dh), g["fc1.b"].data_ptr(), *room, stream)
+        ds.ds_activation_backward(M(self.dh), self.z8.m, ds.DS_ACT_GELU_TANH, M(self.dh), g["fc1.b"], *room, stream)
         self._matmul(M(self.dh.t()), self.normed8.m, M(g["fc1.w"]))
         self._matmul(M(self.dh), M(p["fc1.w"]), M(self.dx))
         room = self._room(ds.ds_layernorm_backward_workspace(self.rows, self.hidden))
-        ds.ds_layernorm_backward(M(self.dx), self.x8.m, self.mean.data_ptr(), self.rstd.data_ptr(), p["gamma"].data_ptr(), ds.DS_BF16,
-                                 M(dy), M(self.dx), g["gamma"].data_ptr(), g["beta"].data_ptr(), *room, stream)
+        ds.ds_layernorm_backward(M(self.dx), self.x8.m, self.mean, self.rstd, p["gamma"], ds.DS_BF16, M(dy), M(self.dx),
+                                 g["gamma"], g["beta"], *room, stream)
         return self.dx
 
     def update(self):

@@ -141,6 +141,7 @@ class ds_matrix(ctypes.Structure):
 
 
 class ds_matmul_epilogue(ctypes.Structure):
+    bias_length = None  # (address, elements) of the tensor that make_epilogue took the bias from
     _fields_ = [
         ("bias", ctypes.c_void_p),
         ("bias_dtype", ctypes.c_uint32),
@@ -767,10 +768,25 @@ def make_mx8(codes, scale) -> ds_matrix:
     return ds_matrix(codes.data_ptr(), DS_MX8, 0, rows, cols, *codes.stride(), scale.data_ptr(), down)
 
 
+def _vector(v, dtype: int, matrix: ds_matrix, axis: str, what: str):
+    """The address of a vector: an address as it is (nothing is known of it, so nothing is checked), or that of a 1-D
+    contiguous torch tensor on the GPU with an element of `dtype` for each of the matrix's rows or cols."""
+    if not hasattr(v, "data_ptr"):
+        return v
+    length = getattr(matrix, axis)
+    if _float_code(v.dtype) != dtype:
+        raise TypeError(f"{what} is {v.dtype}, not of the call's type")
+    if not v.is_cuda:
+        raise ValueError(f"{what} is not in device memory")
+    if v.dim() != 1 or v.shape[0] != length or (length > 1 and v.stride(0) != 1):
+        raise ValueError(f"{what} is {length} elements next to each other, not {tuple(v.shape)} of strides {tuple(v.stride())}")
+    return v.data_ptr()
+
+
 def make_epilogue(bias=None, act: int = DS_ACT_NONE, residual: Optional[ds_matrix] = None,
                   saved: Optional[ds_matrix] = None) -> ds_matmul_epilogue:
-    """`bias`: a 1-D torch tensor on the GPU, contiguous.  (The structure keeps the matrices it points to alive, but no
-    tensor's memory.)"""
+    """`bias`: a 1-D torch tensor on the GPU, contiguous, of c's columns at least.  (The structure keeps the matrices it
+    points to alive, but no tensor's memory.)"""
     ep = ds_matmul_epilogue(None, DS_F32, act)
     if bias is not None:
         ep.bias_dtype = _float_code(bias.dtype)
@@ -779,6 +795,7 @@ def make_epilogue(bias=None, act: int = DS_ACT_NONE, residual: Optional[ds_matri
         if bias.dim() != 1 or (bias.shape[0] > 1 and bias.stride(0) != 1):
             raise ValueError("a bias is one contiguous dimension")
         ep.bias = bias.data_ptr()
+        ep.bias_length = (ep.bias, bias.shape[0])
     if residual is not None:
         ep.residual = ctypes.pointer(residual)
     if saved is not None:
@@ -794,9 +811,13 @@ def ds_mx8_load(saved: ds_matrix, x: ds_matrix, stream: int = 0) -> None:
     _check(_lib.ds_mx8_load(saved, x, stream), "ds_mx8_load")
 
 
-def ds_layernorm_forward(x: ds_matrix, gamma: Optional[int], beta: Optional[int], param_dtype: int, eps: float, y: ds_matrix,
-                         mean: Optional[int] = None, rstd: Optional[int] = None, saved: Optional[ds_matrix] = None,
-                         stream: int = 0) -> None:
+# A vector (gamma, beta, mean, rstd, dgamma, dbeta, dbias) is an address or a torch tensor; of a tensor the length, type and
+# place are checked.
+
+def ds_layernorm_forward(x: ds_matrix, gamma, beta, param_dtype: int, eps: float, y: ds_matrix, mean=None, rstd=None,
+                         saved: Optional[ds_matrix] = None, stream: int = 0) -> None:
+    gamma, beta = _vector(gamma, param_dtype, x, "cols", "gamma"), _vector(beta, param_dtype, x, "cols", "beta")
+    mean, rstd = _vector(mean, DS_F32, x, "rows", "mean"), _vector(rstd, DS_F32, x, "rows", "rstd")
     _check(_lib.ds_layernorm_forward(x, gamma, beta, param_dtype, eps, y, mean, rstd, saved, stream), "ds_layernorm_forward")
 
 
@@ -806,9 +827,11 @@ def ds_layernorm_backward_workspace(rows: int, cols: int) -> int:
     return out.value
 
 
-def ds_layernorm_backward(dy: ds_matrix, x: ds_matrix, mean: int, rstd: int, gamma: Optional[int], param_dtype: int,
-                          residual: Optional[ds_matrix], dx: ds_matrix, dgamma: Optional[int], dbeta: Optional[int],
-                          workspace: Optional[int], workspace_bytes: int, stream: int = 0) -> None:
+def ds_layernorm_backward(dy: ds_matrix, x: ds_matrix, mean, rstd, gamma, param_dtype: int, residual: Optional[ds_matrix],
+                          dx: ds_matrix, dgamma, dbeta, workspace: Optional[int], workspace_bytes: int, stream: int = 0) -> None:
+    mean, rstd = _vector(mean, DS_F32, dy, "rows", "mean"), _vector(rstd, DS_F32, dy, "rows", "rstd")
+    gamma = _vector(gamma, param_dtype, dy, "cols", "gamma")
+    dgamma, dbeta = _vector(dgamma, DS_F32, dy, "cols", "dgamma"), _vector(dbeta, DS_F32, dy, "cols", "dbeta")
     _check(_lib.ds_layernorm_backward(dy, x, mean, rstd, gamma, param_dtype, residual, dx, dgamma, dbeta, workspace,
                                       workspace_bytes, stream), "ds_layernorm_backward")
 
@@ -821,6 +844,10 @@ def ds_matmul_workspace(a: ds_matrix, b: ds_matrix, c: ds_matrix) -> int:
 
 def ds_matmul(a: ds_matrix, b: ds_matrix, c: ds_matrix, epilogue: Optional[ds_matmul_epilogue] = None,
               workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
+    if epilogue is not None and epilogue.bias_length:
+        address, length = epilogue.bias_length
+        if address == epilogue.bias and length < b.cols:
+            raise ValueError(f"the bias has {length} elements for {b.cols} columns")
     _check(_lib.ds_matmul(a, b, c, epilogue, workspace, workspace_bytes, stream), "ds_matmul")
 
 
@@ -830,6 +857,7 @@ def ds_activation_backward_workspace(rows: int, cols: int) -> int:
     return out.value
 
 
-def ds_activation_backward(dy: ds_matrix, z: ds_matrix, act: int, dz: ds_matrix, dbias: Optional[int],
-                           workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
+def ds_activation_backward(dy: ds_matrix, z: ds_matrix, act: int, dz: ds_matrix, dbias, workspace: Optional[int] = None,
+                           workspace_bytes: int = 0, stream: int = 0) -> None:
+    dbias = _vector(dbias, DS_F32, dy, "cols", "dbias")
     _check(_lib.ds_activation_backward(dy, z, act, dz, dbias, workspace, workspace_bytes, stream), "ds_activation_backward")

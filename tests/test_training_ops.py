@@ -234,3 +234,57 @@ def test_math_constants_of_the_tanh_form():
     assert math.isclose(T.act(np.array([1.0]), "gelu_tanh")[0], 0.8411919906082768, rel_tol=1e-12)
     assert math.isclose(T.act(np.array([1.0]), "gelu")[0], 0.8413447460685429, rel_tol=1e-12)
     assert math.isclose(T.act(np.array([1.0]), "silu")[0], 0.7310585786300049, rel_tol=1e-12)
+
+
+class OnGpu:
+    """What the binding looks at of a tensor on the GPU, without one."""
+
+    is_cuda = True
+
+    def __init__(self, t, is_cuda=True):
+        self.t, self.is_cuda, self.shape, self.dtype = t, is_cuda, t.shape, t.dtype
+
+    def dim(self):
+        return self.t.dim()
+
+    def stride(self, k=None):
+        return self.t.stride() if k is None else self.t.stride(k)
+
+    def data_ptr(self):
+        return PTR
+
+
+def test_a_bias_shorter_than_the_columns_is_refused():
+    import torch
+    short, enough = (ds.make_epilogue(bias=OnGpu(torch.zeros(n))) for n in (7, 8))
+    wrong = mat(5, 8)   # refused by the library, so that nothing is launched
+    with pytest.raises(ValueError):
+        ds.ds_matmul(mat(4, 64), mat(64, 8), mat(4, 8), short)
+    assert product(c=wrong, ep=enough) == ds.DS_EINVAL
+    short.bias = PTR + 64   # another vector: nothing is known of it
+    assert product(c=wrong, ep=short) == ds.DS_EINVAL
+
+
+@pytest.mark.parametrize("bad", ("short", "long", "two dimensions", "apart", "host", "type", "no float"))
+def test_vectors_that_do_not_fit_their_matrix(bad):
+    import torch
+
+    def wrong(n, dtype=torch.float32):
+        return {"short": OnGpu(torch.zeros(n - 1, dtype=dtype)), "long": OnGpu(torch.zeros(n + 1, dtype=dtype)),
+                "two dimensions": OnGpu(torch.zeros(1, n, dtype=dtype)), "apart": OnGpu(torch.zeros(2 * n, dtype=dtype)[::2]),
+                "host": torch.zeros(n, dtype=dtype), "type": OnGpu(torch.zeros(n, dtype=torch.float16)),
+                "no float": OnGpu(torch.zeros(n, dtype=torch.int32))}[bad]
+
+    kind = TypeError if bad in ("type", "no float") else ValueError
+    for name, n, dtype in (("gamma", 64, torch.bfloat16), ("beta", 64, torch.bfloat16), ("mean", 4, torch.float32), ("rstd", 4, torch.float32)):
+        with pytest.raises(kind):
+            forward(**{name: wrong(n, dtype)})
+        assert forward(y=mat(5, 64), **{name: OnGpu(torch.zeros(n, dtype=dtype))}) == ds.DS_EINVAL
+    for name, n, dtype in (("gamma", 64, torch.bfloat16), ("dgamma", 64, torch.float32), ("dbeta", 64, torch.float32), ("mean", 4, torch.float32),
+                           ("rstd", 4, torch.float32)):
+        with pytest.raises(kind):
+            backward(**{name: wrong(n, dtype)})
+        assert backward(dx=mat(5, 64), **{name: OnGpu(torch.zeros(n, dtype=dtype))}) == ds.DS_EINVAL
+    with pytest.raises(kind):
+        act_back(dbias=wrong(64))
+    assert act_back(dz=mat(5, 64), dbias=OnGpu(torch.zeros(64))) == ds.DS_EINVAL
