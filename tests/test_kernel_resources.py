@@ -120,3 +120,29 @@ def test_the_digest_that_profiles_name_covers_the_flags(monkeypatch):
     assert ds.kernel_source_digest() == before
     monkeypatch.setattr(build, "HIPCC_FLAGS", [f for f in build.HIPCC_FLAGS if "preload" not in f])
     assert ds.kernel_source_digest() != before
+
+
+def _instructions(elf, path):
+    path.write_bytes(elf)
+    out = subprocess.run(["/opt/rocm/llvm/bin/llvm-objdump", "-d", "--no-show-raw-insn", "--no-leading-addr", str(path)], capture_output=True,
+                         text=True, check=True).stdout
+    return [line.split("//")[0].strip() for line in out.splitlines() if line.startswith("\t")]
+
+
+def test_loads_to_lds_wait_for_the_scalar_registers_they_read(tmp_path):
+    """Loads to LDS are written in assembly, into which the compiler does not look for hazards: a scalar register that a vector
+    instruction has written may be read by a load five wait states later at the earliest.  Whatever is scheduled in front of
+    them, five wait states are part of the assembly."""
+    if not os.path.exists(LIB):
+        pytest.skip("the library is not built")
+    with open(LIB, "rb") as f:
+        blob = f.read()
+    loads = 0
+    for elf in _code_objects(blob):
+        code = _instructions(elf, tmp_path / "elf")
+        for i, line in enumerate(code):
+            if line.startswith("buffer_load") and line.endswith(" lds"):
+                loads += 1
+                wait = re.fullmatch(r"s_nop (\d+)", code[i - 1])
+                assert wait and int(wait.group(1)) >= 4, code[i - 5:i + 1]
+    assert loads >= 48
