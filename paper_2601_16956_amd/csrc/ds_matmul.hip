@@ -218,9 +218,10 @@ struct TileArgs {
 // Written by hand because the compiler would otherwise wait for the transfers of the next stage before it reads this one.  It does not
 // look into the assembly for hazards either: a load may read a scalar register that a vector instruction has written (the resource's,
 // by v_readfirstlane) five wait states later at the earliest, and m0 one.  (They cost nothing that can be measured.)
+// m0 is an operand, so that the compiler writes it: it takes m0 to keep what it wrote there, and heeds no clobber of it.
 constexpr uint32_t kNowhere = 0x80000000u;
 __device__ inline void to_lds(uint32_t lds, uint32_t offset, u32x4 resource) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(resource) : "memory");
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(lds), "v"(offset), "s"(resource) : "memory");
 }
 // All but the last LATER transfers of this wavefront are done, and what it has read of LDS is in registers; then the same
 // holds for the work-group.

@@ -146,3 +146,19 @@ def test_loads_to_lds_wait_for_the_scalar_registers_they_read(tmp_path):
                 wait = re.fullmatch(r"s_nop (\d+)", code[i - 1])
                 assert wait and int(wait.group(1)) >= 4, code[i - 5:i + 1]
     assert loads >= 48
+
+
+def test_no_inline_assembly_writes_m0():
+    """The compiler takes m0 to keep what it wrote there, and a clobber list is not heeded for it: a value for m0 is an operand
+    ("{m0}"), which the compiler moves there itself."""
+    csrc = os.path.join(ROOT, "paper_2601_16956_amd", "csrc")
+    uses = 0
+    for name in sorted(os.listdir(csrc)):
+        with open(os.path.join(csrc, name)) as f:
+            text = f.read()
+        for code in re.findall(r"\basm\s+(?:volatile\s*)?\((.*?)\);", text, re.S):
+            assert not re.search(r"\bs_\w+\s+m0\b", code), (name, code)
+            if re.search(r"\blds\b", code):
+                assert '"{m0}"(' in code, (name, code)
+                uses += 1
+    assert uses >= 1
