@@ -771,7 +771,7 @@ def make_mx8(codes, scale) -> ds_matrix:
 def _vector(v, dtype: int, matrix: ds_matrix, axis: str, what: str):
     """The address of a vector: an address as it is (nothing is known of it, so nothing is checked), or that of a 1-D
     contiguous torch tensor on the GPU with an element of `dtype` for each of the matrix's rows or cols."""
-    if not hasattr(v, "data_ptr"):
+    if v is None or type(v) is int or not hasattr(v, "data_ptr"):
         return v
     length = getattr(matrix, axis)
     if _float_code(v.dtype) != dtype:
@@ -794,8 +794,8 @@ def make_epilogue(bias=None, act: int = DS_ACT_NONE, residual: Optional[ds_matri
             raise ValueError("the bias is not in device memory")
         if bias.dim() != 1 or (bias.shape[0] > 1 and bias.stride(0) != 1):
             raise ValueError("a bias is one contiguous dimension")
-        ep.bias = bias.data_ptr()
-        ep.bias_length = (ep.bias, bias.shape[0])
+        ep.bias = address = bias.data_ptr()
+        ep.bias_length = (address, bias.shape[0])
     if residual is not None:
         ep.residual = ctypes.pointer(residual)
     if saved is not None:
