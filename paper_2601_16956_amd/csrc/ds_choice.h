@@ -1,0 +1,101 @@
+// How ds_matmul computes a product: host arithmetic on sizes, strides and alignment, without a device.
+#pragma once
+
+#include <stdint.h>
+
+#include "datastates.h"
+
+namespace {
+
+// An operand: element (p, k), p a row of a or a column of b.
+struct Operand {
+  const void *base;
+  int64_t ld;      // elements from p to p + 1 (k_last), or from k to k + 1
+  int64_t extent;  // of p
+  const uint8_t *scale;
+  int64_t scale_stride;
+  bool k_last;  // neighbouring k are neighbours in memory
+};
+
+// a (or b's transpose): p along `along` = its rows if `p_rows`.
+inline Operand operand(const ds_matrix *m, bool p_rows) {
+  const int64_t p = p_rows ? m->rows : m->cols, k = p_rows ? m->cols : m->rows;
+  const int64_t step_p = p_rows ? m->row_stride : m->col_stride, step_k = p_rows ? m->col_stride : m->row_stride;
+  // in rows if the columns are neighbours; a matrix of one row or column may be either
+  const bool in_rows = (m->cols <= 1 || m->col_stride == 1) && (m->rows <= 1 || m->row_stride >= m->cols);
+  const bool k_last = in_rows == p_rows;
+  const int64_t ld = k_last ? (p > 1 ? step_p : k) : (k > 1 ? step_k : p);
+  return Operand{m->base, ld, p, m->dtype == DS_MX8 ? m->scale : nullptr, m->scale_stride, k_last};
+}
+
+constexpr int kStep = 64;  // of k: what a stage of LDS holds, twice what a matrix instruction takes
+constexpr int kFewRows = 16;  // rows of a that the kernel for few rows takes
+
+enum class Way { kSimple, kTile, kFew };
+struct Choice {
+  Way way;
+  int tile;         // index into kTiles
+  uint32_t splits;
+  bool lines_a, lines_b;  // is the operand laid out in the workspace first?
+  uint64_t at_a, at_b, at_partial, bytes;
+};
+// A tile's extents, how many of its work-groups a CU holds, and what they take, in us: before and behind the steps; a step where most
+// CUs are idle; a step with 1, 2, 3 work-groups on every CU.  (Measured with bfloat16 [out, in] on products of 4 to 256 steps; what
+// the steps take on a full chip is decided by its power.)
+struct TileSize {
+  int m, n, at_once;
+  double around, idle, step[3];
+};
+constexpr TileSize kTiles[] = {
+    {256, 256, 1, 9.9, 0.96, {1.41}},       {192, 256, 1, 8.6, 0.78, {1.20}},
+    {128, 256, 1, 7.1, 0.56, {0.80}},       {128, 128, 1, 5.6, 0.36, {0.55}},
+    {64, 128, 2, 5.2, 0.295, {0.33, 0.66}}, {64, 64, 3, 4.7, 0.255, {0.27, 0.36, 0.70}},
+};
+constexpr int64_t kCus = 256;
+inline double tile_time(const TileSize &s, int64_t m, int64_t n, int64_t steps, int64_t splits) {
+  const int64_t groups = (m + s.m - 1) / s.m * ((n + s.n - 1) / s.n) * splits, each = (steps + splits - 1) / splits;
+  const int64_t on_cu = (groups + kCus - 1) / kCus, rounds = (on_cu + s.at_once - 1) / s.at_once, rest = on_cu % s.at_once;
+  double step = (double)(on_cu / s.at_once) * s.step[s.at_once - 1] + (rest ? s.step[rest - 1] : 0.0);
+  if (on_cu == 1) step = s.idle + (s.step[0] - s.idle) * (double)groups / kCus;
+  // a further round's beginning and end; those of work-groups that share a CU overlap
+  double t = s.around + (double)each * step + (double)(rounds - 1) * (s.around - 3.0);
+  if (splits > 1) t += 4.0 + (double)m * (double)n * (double)splits * 8.0 / 5e6;  // the sums' way through memory, and a launch
+  return t;
+}
+
+// May the operand be read in 16-byte pieces, all within its lines?
+inline bool in_pieces(const Operand &o, int64_t depth) {
+  const int64_t length = o.k_last ? depth : o.extent;
+  return !o.scale && ((uintptr_t)o.base & 15) == 0 && length % 8 == 0 && (o.ld % 8 == 0) && o.ld < (1 << 21);
+}
+inline uint64_t lines_bytes(const Operand &o, int64_t depth) {
+  const int64_t lines = o.k_last ? o.extent : depth, length = o.k_last ? depth : o.extent;
+  return (uint64_t)(lines * ((length + 7) / 8 * 8) * 2 + 127) / 128 * 128;
+}
+
+inline Choice choose(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t depth) {
+  Choice c{Way::kSimple, 0, 1, false, false, 0, 0, 0, 0};
+  // lines of 16-bit values are at most 2^22 bytes apart, so that a stage's offsets have 31 bits
+  const auto too_long = [&](const Operand &o) { return (o.k_last ? depth : o.extent) > (1 << 21); };
+  if (depth == 0) return c;
+  if (m <= kFewRows && a.k_last && b.k_last && !a.scale && !b.scale) {
+    c.way = Way::kFew;
+    return c;
+  }
+  if (m * n * depth < (1 << 18) || too_long(a) || too_long(b)) return c;
+  c.way = Way::kTile;
+  c.lines_a = !in_pieces(a, depth), c.lines_b = !in_pieces(b, depth);
+  const int64_t steps = (depth + kStep - 1) / kStep;
+  double best = 1e300;
+  for (int i = 0; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i)
+    for (int64_t splits = 1; splits <= 16 && splits * 4 <= steps + 3; ++splits) {
+      const double time = tile_time(kTiles[i], m, n, steps, splits);
+      if (time < best) best = time, c.tile = i, c.splits = (uint32_t)splits;
+    }
+  if (c.lines_a) c.at_a = c.bytes, c.bytes += lines_bytes(a, depth);
+  if (c.lines_b) c.at_b = c.bytes, c.bytes += lines_bytes(b, depth);
+  if (c.splits > 1) c.at_partial = c.bytes, c.bytes += (uint64_t)c.splits * m * n * 4;
+  return c;
+}
+
+}  // namespace

@@ -1,0 +1,82 @@
+"""Which kernel a product takes, asked of the library's own rule, and every kernel of tiles whole and split along k."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+import paper_2601_16956_amd as ds
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+BASE = 0x100000   # never dereferenced
+
+# (m, k, n): the tile and the splits that are chosen
+WHOLE = {(3904, 520, 3904): (256, 256), (3900, 515, 3901): (256, 256), (2752, 328, 4096): (192, 256), (2750, 333, 4090): (192, 256),
+         (1984, 200, 3992): (128, 256), (1990, 203, 3990): (128, 256), (1504, 600, 2000): (128, 128), (1500, 601, 2001): (128, 128),
+         (704, 5000, 2104): (64, 128), (700, 5001, 2100): (64, 128), (1104, 496, 1304): (64, 64)}
+SPLIT = {(3632, 8192, 1032): (256, 256, 3), (3630, 8189, 1037): (256, 256, 3), (2696, 8192, 824): (192, 256, 4), (4593, 13098, 1150): (192, 256, 2),
+         (200, 8192, 4152): (128, 256, 7), (201, 8191, 4149): (128, 256, 7), (200, 4096, 2696): (128, 128, 5), (2252, 11021, 377): (128, 128, 4),
+         (304, 16384, 304): (64, 128, 16), (130, 3001, 2750): (64, 128, 3), (600, 3000, 704): (64, 64, 4), (130, 2049, 130): (64, 64, 9)}
+
+
+@pytest.fixture(scope="module")
+def choose(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("choice") / "choice_host.so")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-Wall", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-static-libubsan", "-fPIC", "-shared",
+                    "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2601_16956_amd", "csrc"),
+                    os.path.join(ROOT, "tests", "c_abi", "choice_host.cpp"), "-o", so], check=True)
+    fn = ctypes.CDLL(so).choice_host
+    fn.argtypes = [ctypes.POINTER(ds.ds_matrix), ctypes.POINTER(ds.ds_matrix), ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_uint64 * 7)]
+
+    def ask(a, b, c):
+        out = (ctypes.c_uint64 * 7)()
+        fn(a, b, c.rows, c.cols, out)
+        return dict(zip(("way", "m", "n", "splits", "lines_a", "lines_b", "bytes"), out), way=("simple", "tiles", "few rows")[out[0]])
+    return ask
+
+
+def matrices(m, k, n, layout="nt", kind=ds.DS_BF16, base=BASE, pad=0):
+    def one(rows, cols, transposed):
+        if transposed:
+            return ds.ds_matrix(base, kind, 0, rows, cols, 1, rows + pad, None, 0)
+        return ds.ds_matrix(base, kind, 0, rows, cols, cols + pad, 1, None, 0)
+    return one(m, k, layout[0] == "t"), one(k, n, layout[1] == "t"), ds.ds_matrix(base, ds.DS_F32, 0, m, n, n, 1, None, 0)
+
+
+@pytest.mark.parametrize("layout", ("nt", "nn", "tn", "tt"))
+def test_the_sizes_below_reach_every_tile_whole_and_split(choose, layout):
+    for sizes, want in (*WHOLE.items(), *SPLIT.items()):
+        c = choose(*matrices(*sizes, layout))
+        assert c["way"] == "tiles" and (c["m"], c["n"], c["splits"]) == (want if len(want) == 3 else (*want, 1)), (sizes, c)
+    tiles = {(256, 256), (192, 256), (128, 256), (128, 128), (64, 128), (64, 64)}
+    assert set(WHOLE.values()) == tiles and {t[:2] for t in SPLIT.values()} == tiles
+    # splits of k whose steps of 64 are not as many for each
+    assert {t[:2] for (_, k, _), t in SPLIT.items() if -(-k // 64) % t[2]} == tiles
+
+
+def test_the_workspace_is_what_the_choice_needs(choose):
+    for sizes in (*WHOLE, *SPLIT, (1, 4096, 64), (16, 8192, 300), (3, 5, 7), (17, 31, 65)):
+        for layout in ("nt", "nn", "tn", "tt"):
+            for base, pad in ((BASE, 0), (BASE + 2, 0), (BASE, 4)):
+                a, b, c = matrices(*sizes, layout, base=base, pad=pad)
+                if base != BASE:
+                    c.base = BASE
+                how = choose(a, b, c)
+                assert ds.ds_matmul_workspace(a, b, c) == how["bytes"]
+                if how["way"] != "tiles":
+                    assert how["bytes"] == 0
+
+
+def test_few_rows_and_small_products_have_ways_of_their_own(choose):
+    assert choose(*matrices(1, 8192, 3584))["way"] == choose(*matrices(16, 100, 33))["way"] == "few rows"
+    assert choose(*matrices(17, 8192, 3584))["way"] == choose(*matrices(1, 8192, 3584, "nn"))["way"] == "tiles"
+    assert choose(*matrices(33, 100, 40))["way"] == choose(*matrices(70, 0, 40))["way"] == "simple"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ("nt", "nn", "tn", "tt"))
+@pytest.mark.parametrize("sizes", SPLIT)
+def test_products_of_every_tile_split_along_k(sizes, layout):
+    """Against products in 64 bits, within bounds derived from the roundings."""
+    import test_gpu_training_ops as ops
+    ops.test_matmul_of_every_tile(*sizes, layout)
