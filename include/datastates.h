@@ -623,8 +623,11 @@ int ds_ckpt_restore_parts(const ds_ckpt_reader *const *readers, uint32_t n_parts
  *   - All are asynchronous on `stream`, allocate nothing, keep nothing between
  *     calls and may be captured into a graph.  A workspace is device memory of
  *     the caller, 16-byte aligned, of the size that the function's _workspace
- *     partner names for the same sizes; it may be used by the next call on the
- *     same stream at once, and its contents mean nothing afterwards.
+ *     partner names for the same arguments (ds_matmul_workspace: the same
+ *     matrices; types, strides and alignment count, not the extents alone, so
+ *     that a slice may need what its whole does not); it may be used by the
+ *     next call on the same stream at once, and its contents mean nothing
+ *     afterwards.
  *   - Results do not depend on timing: the same call on the same inputs gives
  *     the same bytes.
  *   - Sums, statistics and products are accumulated in 32 bits; a result is

@@ -837,6 +837,7 @@ def ds_layernorm_backward(dy: ds_matrix, x: ds_matrix, mean, rstd, gamma, param_
 
 
 def ds_matmul_workspace(a: ds_matrix, b: ds_matrix, c: ds_matrix) -> int:
+    """Bytes for ds_matmul of these matrices: strides and alignment count, not the extents alone."""
     out = ctypes.c_uint64(0)
     _check(_lib.ds_matmul_workspace(a, b, c, out), "ds_matmul_workspace")
     return out.value

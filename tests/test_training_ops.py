@@ -288,3 +288,25 @@ def test_vectors_that_do_not_fit_their_matrix(bad):
     with pytest.raises(kind):
         act_back(dbias=wrong(64))
     assert act_back(dz=mat(5, 64), dbias=OnGpu(torch.zeros(64))) == ds.DS_EINVAL
+
+
+@pytest.mark.parametrize("what", ("lines laid out", "split along k", "both"))
+def test_a_product_s_workspace_too_small_missing_or_misaligned(what):
+    pad = 0 if what == "split along k" else 4
+    m, k, n = (256, 512, 256) if what == "lines laid out" else (304, 16384, 304)
+    a, b, c = mat(m, k, row=k + pad), mat(k, n), mat(m, n)
+    need = ds.ds_matmul_workspace(a, b, c)
+    assert need >= (m * k * 2 if pad else 0) + (2 * m * n * 4 if what != "lines laid out" else 0) > 0
+    assert product(a, b, c, size=need - 1) == product(a, b, c, size=0) == ds.DS_ERANGE
+    assert product(a, b, c, ws=None, size=need) == product(a, b, c, ws=None, size=0) == ds.DS_EINVAL
+    for off in (1, 2, 4, 8):
+        assert product(a, b, c, ws=PTR + off, size=need) == ds.DS_EINVAL
+
+
+def test_a_product_s_workspace_goes_by_strides_and_alignment():
+    m, k, n = 256, 512, 256
+    b, c = mat(k, n), mat(m, n)
+    assert ds.ds_matmul_workspace(mat(m, k), b, c) == 0
+    for a in (mat(m, k, base=PTR + 2), mat(m, k, row=k + 4), mat(m, k, ds.DS_MX8)):
+        assert ds.ds_matmul_workspace(a, b, c) == m * k * 2
+        assert product(a, b, c, ws=None, size=0) == ds.DS_EINVAL
