@@ -726,7 +726,8 @@ typedef struct ds_matmul_epilogue {
  * are then rounded to the other's type (to DS_BF16 if both are DS_MX8), which is
  * exact for a checkpoint of that type.  c: DS_F32, DS_BF16 or DS_F16, ROWS.  epilogue: NULL = all of it absent.
  * With k = 0 the product is zero.  Errors: DS_EINVAL, DS_ERANGE (an extent
- * beyond 2^31 - 1 or a workspace too small), DS_EHIP.
+ * beyond 2^31 - 1, more than 2^22 tiles of c, of 64 x 64 elements at least,
+ * which both functions refuse, or a workspace too small), DS_EHIP.
  */
 int ds_matmul_workspace(const ds_matrix *a, const ds_matrix *b, const ds_matrix *c, uint64_t *bytes);
 int ds_matmul(const ds_matrix *a, const ds_matrix *b, const ds_matrix *c, const ds_matmul_epilogue *epilogue,

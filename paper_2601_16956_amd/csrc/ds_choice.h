@@ -31,7 +31,9 @@ inline Operand operand(const ds_matrix *m, bool p_rows) {
 constexpr int kStep = 64;  // of k: what a stage of LDS holds, twice what a matrix instruction takes
 constexpr int kFewRows = 16;  // rows of a that the kernel for few rows takes
 
-enum class Way { kSimple, kTile, kFew };
+constexpr int64_t kMaxTiles = 1 << 22;  // work-groups of a launch
+
+enum class Way { kSimple, kTile, kFew, kNone };  // kNone: there are too many tiles for any
 struct Choice {
   Way way;
   int tile;         // index into kTiles
@@ -52,8 +54,9 @@ constexpr TileSize kTiles[] = {
     {64, 128, 2, 5.2, 0.295, {0.33, 0.66}}, {64, 64, 3, 4.7, 0.255, {0.27, 0.36, 0.70}},
 };
 constexpr int64_t kCus = 256;
+inline int64_t tiles_of(int64_t m, int64_t n, int64_t tile_m, int64_t tile_n) { return (m + tile_m - 1) / tile_m * ((n + tile_n - 1) / tile_n); }
 inline double tile_time(const TileSize &s, int64_t m, int64_t n, int64_t steps, int64_t splits) {
-  const int64_t groups = (m + s.m - 1) / s.m * ((n + s.n - 1) / s.n) * splits, each = (steps + splits - 1) / splits;
+  const int64_t groups = tiles_of(m, n, s.m, s.n) * splits, each = (steps + splits - 1) / splits;
   const int64_t on_cu = (groups + kCus - 1) / kCus, rounds = (on_cu + s.at_once - 1) / s.at_once, rest = on_cu % s.at_once;
   double step = (double)(on_cu / s.at_once) * s.step[s.at_once - 1] + (rest ? s.step[rest - 1] : 0.0);
   if (on_cu == 1) step = s.idle + (s.step[0] - s.idle) * (double)groups / kCus;
@@ -70,28 +73,29 @@ inline bool in_pieces(const Operand &o, int64_t depth) {
 }
 inline uint64_t lines_bytes(const Operand &o, int64_t depth) {
   const int64_t lines = o.k_last ? o.extent : depth, length = o.k_last ? depth : o.extent;
-  return (uint64_t)(lines * ((length + 7) / 8 * 8) * 2 + 127) / 128 * 128;
+  return ((uint64_t)lines * (uint64_t)((length + 7) / 8 * 8) * 2 + 127) / 128 * 128;
 }
 
 inline Choice choose(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t depth) {
-  Choice c{Way::kSimple, 0, 1, false, false, 0, 0, 0, 0};
+  Choice c{tiles_of(m, n, 64, 64) <= kMaxTiles ? Way::kSimple : Way::kNone, 0, 1, false, false, 0, 0, 0, 0};
   // lines of 16-bit values are at most 2^22 bytes apart, so that a stage's offsets have 31 bits
   const auto too_long = [&](const Operand &o) { return (o.k_last ? depth : o.extent) > (1 << 21); };
   if (depth == 0) return c;
-  if (m <= kFewRows && a.k_last && b.k_last && !a.scale && !b.scale) {
+  if (m <= kFewRows && a.k_last && b.k_last && !a.scale && !b.scale && n <= kMaxTiles * 32) {
     c.way = Way::kFew;
     return c;
   }
-  if (m * n * depth < (1 << 18) || too_long(a) || too_long(b)) return c;
-  c.way = Way::kTile;
-  c.lines_a = !in_pieces(a, depth), c.lines_b = !in_pieces(b, depth);
+  if ((double)m * (double)n * (double)depth < (1 << 18) || too_long(a) || too_long(b)) return c;
   const int64_t steps = (depth + kStep - 1) / kStep;
   double best = 1e300;
   for (int i = 0; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i)
     for (int64_t splits = 1; splits <= 16 && splits * 4 <= steps + 3; ++splits) {
+      if (tiles_of(m, n, kTiles[i].m, kTiles[i].n) * splits > kMaxTiles) break;
       const double time = tile_time(kTiles[i], m, n, steps, splits);
-      if (time < best) best = time, c.tile = i, c.splits = (uint32_t)splits;
+      if (time < best) best = time, c.way = Way::kTile, c.tile = i, c.splits = (uint32_t)splits;
     }
+  if (c.way != Way::kTile) return c;
+  c.lines_a = !in_pieces(a, depth), c.lines_b = !in_pieces(b, depth);
   if (c.lines_a) c.at_a = c.bytes, c.bytes += lines_bytes(a, depth);
   if (c.lines_b) c.at_b = c.bytes, c.bytes += lines_bytes(b, depth);
   if (c.splits > 1) c.at_partial = c.bytes, c.bytes += (uint64_t)c.splits * m * n * 4;

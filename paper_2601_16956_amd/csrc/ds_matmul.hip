@@ -27,6 +27,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
+static_assert(kMaxTiles <= kMaxGrid && kMaxTiles * 512 < (int64_t)1 << 32, "a launch's threads");
 
 struct Epilogue {
   Rows c, residual, saved;
@@ -682,7 +683,9 @@ int launch_product(const Operand &a, const Operand &b, const Epilogue &e, int64_
 extern "C" int ds_matmul_workspace(const ds_matrix *a, const ds_matrix *b, const ds_matrix *c, uint64_t *bytes) {
   if (!bytes) return DS_EINVAL;
   DS_TRY(check_product(a, b, c));
-  *bytes = choose(operand(a, true), operand(b, false), c->rows, c->cols, a->cols).bytes;
+  const Choice how = choose(operand(a, true), operand(b, false), c->rows, c->cols, a->cols);
+  if (how.way == Way::kNone) return DS_ERANGE;
+  *bytes = how.bytes;
   return DS_OK;
 }
 
@@ -703,13 +706,12 @@ extern "C" int ds_matmul(const ds_matrix *a, const ds_matrix *b, const ds_matrix
   if (c->rows == 0 || c->cols == 0) return DS_OK;
   const Operand oa = operand(a, true), ob = operand(b, false);
   const Choice how = choose(oa, ob, c->rows, c->cols, a->cols);
+  if (how.way == Way::kNone) return DS_ERANGE;
   if (how.bytes) {
     if (!workspace || ds_misaligned(workspace, 16)) return DS_EINVAL;
     if (workspace_bytes < how.bytes) return DS_ERANGE;
   }
   const Epilogue e{ds_rows(c), ds_rows(ep.residual), ds_rows(ep.saved), ep.bias, c->rows, c->cols, c->dtype, ep.bias_dtype, ep.act};
-  // work-groups of a launch: of 64 x 64, the smallest tile
-  if (((c->rows + 63) / 64) * ((c->cols + 63) / 64) > kMaxGrid) return DS_ERANGE;
   if (a->dtype == DS_F16 || b->dtype == DS_F16)
     return launch_product<__half>(oa, ob, e, a->cols, how, (uint8_t *)workspace, (hipStream_t)stream);
   return launch_product<__hip_bfloat16>(oa, ob, e, a->cols, how, (uint8_t *)workspace, (hipStream_t)stream);

@@ -31,7 +31,7 @@ def choose(tmp_path_factory):
     def ask(a, b, c):
         out = (ctypes.c_uint64 * 7)()
         fn(a, b, c.rows, c.cols, out)
-        return dict(zip(("way", "m", "n", "splits", "lines_a", "lines_b", "bytes"), out), way=("simple", "tiles", "few rows")[out[0]])
+        return dict(zip(("way", "m", "n", "splits", "lines_a", "lines_b", "bytes"), out), way=("simple", "tiles", "few rows", "none")[out[0]])
     return ask
 
 
@@ -71,6 +71,52 @@ def test_few_rows_and_small_products_have_ways_of_their_own(choose):
     assert choose(*matrices(1, 8192, 3584))["way"] == choose(*matrices(16, 100, 33))["way"] == "few rows"
     assert choose(*matrices(17, 8192, 3584))["way"] == choose(*matrices(1, 8192, 3584, "nn"))["way"] == "tiles"
     assert choose(*matrices(33, 100, 40))["way"] == choose(*matrices(70, 0, 40))["way"] == "simple"
+
+
+FAR = (1 << 31) - 1
+WIDE = [(1, 8, (1 << 28) + 128), (16, 8, FAR), (1, 1 << 14, FAR), (FAR, 3, 8), (FAR, 0, 64), (FAR, 8, FAR), (1 << 18, 64, 1 << 20), (FAR, FAR, FAR),
+        (1 << 14, 8, (1 << 21) + 8), (1 << 18, 8, (1 << 21) + 8), (FAR, 1 << 20, 1 << 10), (64, FAR, 64), (FAR, 1, FAR), (1, FAR, 1)]
+
+
+@pytest.mark.parametrize("layout", ("nt", "nn", "tn", "tt"))
+@pytest.mark.parametrize("sizes", WIDE)
+def test_products_of_far_extents_fit_a_launch_or_are_refused_by_both(choose, sizes, layout):
+    """(The choice is compiled with checks of its arithmetic, which fail on an overflow.)"""
+    m, k, n = sizes
+    a, b, c = matrices(m, k, n, layout)
+    how = choose(a, b, c)
+    if how["way"] == "none":
+        assert -(-m // 64) * -(-n // 64) > 1 << 22
+        for call in (lambda: ds.ds_matmul_workspace(a, b, c), lambda: ds.ds_matmul(a, b, c, None, BASE, 1 << 62)):
+            with pytest.raises(ds.DsError) as e:
+                call()
+            assert e.value.code == ds.DS_ERANGE
+        return
+    rows, cols, threads = {"few rows": (m, 32, 512), "simple": (64, 64, 256), "tiles": (how["m"], how["n"], 512)}[how["way"]]
+    assert -(-m // rows) * -(-n // cols) * how["splits"] * threads < 1 << 32
+    lines = sum(2 * p * -(-length // 8) * 8 for out, p, length in (
+        (how["lines_a"], *((k, m) if layout[0] == "t" else (m, k))), (how["lines_b"], *((n, k) if layout[1] == "t" else (k, n)))) if out)
+    partial = 4 * how["splits"] * m * n if how["splits"] > 1 else 0
+    assert lines + partial <= how["bytes"] <= lines + partial + 256 and how["bytes"] == ds.ds_matmul_workspace(a, b, c)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [(1 << 27), (1 << 28) + 136])
+def test_a_product_of_a_row_with_more_columns_than_one_launch_takes(n):
+    """Whole numbers, so that sums are exact in any order."""
+    import torch
+    import test_gpu_training_ops as ops
+    a = torch.tensor([[3, -2, 5, 1, 0, 7, -4, 2]], device="cuda").bfloat16()
+    b = torch.randint(-9, 10, (n, 8), device="cuda", dtype=torch.int8).bfloat16()
+    c = torch.empty(1, n, dtype=torch.float32, device="cuda")
+    A, B, C = ds.make_matrix(a), ds.make_matrix(b.t()), ds.make_matrix(c)
+    need = ds.ds_matmul_workspace(A, B, C)
+    ws, whole = ops.workspace(need)
+    ds.ds_matmul(A, B, C, None, ws.data_ptr(), need, ops.stream())
+    for first in range(0, n, 1 << 26):
+        part = b[first:first + (1 << 26)].float()
+        assert torch.equal(c[0, first:first + (1 << 26)], sum(part[:, i] * a[0, i].float() for i in range(8)))
+    assert whole()
 
 
 @pytest.mark.gpu
