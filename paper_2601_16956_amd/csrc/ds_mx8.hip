@@ -102,30 +102,33 @@ __global__ __launch_bounds__(kThreads) void ds_activation_backward_kernel(Rows d
   }
 }
 
-// The lines of `partial` added: a work-group has 16 columns, and each of its 16 rows of threads every 16th line; then those 16 sums
-// in their order.  blockIdx.y: the first or the second set of lines.
+// The lines of `partial` added: a work-group has 16 columns (and further ones where a launch has no place for as many work-groups), and each
+// of its 16 rows of threads every 16th line; then those 16 sums in their order.  blockIdx.y: the first or the second set of lines.
 __global__ __launch_bounds__(kThreads) void ds_sum_parts_kernel(const float *partial, int64_t parts, int64_t cols, float *out0, float *out1) {
   __shared__ float sums[16][16 + 1];
   const int across = threadIdx.x % 16, row = threadIdx.x / 16;
-  const int64_t j = (int64_t)blockIdx.x * 16 + across;
   float *out = blockIdx.y ? out1 : out0;
-  const float *from = partial + blockIdx.y * parts * cols + j;
   if (!out) return;
-  float sum[4] = {};
-  if (j < cols) {
-    int64_t p = row;
-    for (; p + 48 < parts; p += 64)
+  for (int64_t first = (int64_t)blockIdx.x * 16; first < cols; first += (int64_t)gridDim.x * 16) {
+    const int64_t j = first + across;
+    const float *from = partial + blockIdx.y * parts * cols + j;
+    float sum[4] = {};
+    if (j < cols) {
+      int64_t p = row;
+      for (; p + 48 < parts; p += 64)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) sum[u] += from[(p + 16 * u) * cols];
-    for (; p < parts; p += 16) sum[0] += from[p * cols];
-  }
-  sums[row][across] = sum[0] + sum[1] + (sum[2] + sum[3]);
-  __syncthreads();
-  if (row == 0 && j < cols) {
-    float s = 0.f;
+        for (int u = 0; u < 4; ++u) sum[u] += from[(p + 16 * u) * cols];
+      for (; p < parts; p += 16) sum[0] += from[p * cols];
+    }
+    sums[row][across] = sum[0] + sum[1] + (sum[2] + sum[3]);
+    __syncthreads();
+    if (row == 0 && j < cols) {
+      float s = 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s += sums[r][across];
-    out[j] = s;
+      for (int r = 0; r < 16; ++r) s += sums[r][across];
+      out[j] = s;
+    }
+    __syncthreads();
   }
 }
 
@@ -191,8 +194,9 @@ int64_t act_parts(int64_t rows, int64_t cols) {
 }  // namespace
 
 int ds_launch_sum_parts(const float *partial, int64_t parts, int64_t cols, float *out0, float *out1, hipStream_t stream) {
-  hipLaunchKernelGGL(ds_sum_parts_kernel, dim3((uint32_t)((cols + 15) / 16), out1 ? 2 : 1), dim3(kThreads), 0, stream, partial, parts, cols,
-                     out0, out1);
+  const int64_t groups = (cols + 15) / 16;
+  hipLaunchKernelGGL(ds_sum_parts_kernel, dim3((uint32_t)(groups < kMaxGrid ? groups : kMaxGrid), out1 ? 2 : 1), dim3(kThreads), 0, stream, partial,
+                     parts, cols, out0, out1);
   DS_HIP_TRY(hipGetLastError());
   return DS_OK;
 }

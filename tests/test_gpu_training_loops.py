@@ -191,3 +191,24 @@ def test_checkpoints_of_many_pieces(rows, cols, kind):
     ds.ds_mx8_load(ds.make_mx8(q, s), ds.make_matrix(back), stream())
     want_q, want_s = encode(x.double())
     assert torch.equal(q, want_q) and torch.equal(s, want_s) and torch.equal(back.double(), decode(q, s))
+
+
+@pytest.mark.parametrize("cols", [(1 << 26) + 40, (1 << 28) + 40])
+def test_sums_over_rows_of_more_columns_than_a_launch_has_work_groups_for(cols):
+    """Two rows, so that the sums are one addition."""
+    dy = torch.randint(-100, 101, (2, cols), device="cuda", dtype=torch.int8).bfloat16()
+    dy *= 0.37
+    want = dy[0].float() + dy[1].float()
+    need = ds.ds_activation_backward_workspace(2, cols)
+    (ws, whole), dbias = workspace(need), torch.full((cols,), 5.0, device="cuda")
+    M = ds.make_matrix(dy)
+    ds.ds_activation_backward(M, M, ds.DS_ACT_NONE, M, dbias, ws.data_ptr(), need, stream())
+    assert torch.equal(dbias, want) and whole()
+    del ws, whole
+    need = ds.ds_layernorm_backward_workspace(2, cols)
+    (ws, whole), dbeta, dgamma = workspace(need), torch.full((cols,), 5.0, device="cuda"), torch.full((cols,), 5.0, device="cuda")
+    mean, rstd = torch.tensor([1.0, -2.0], device="cuda"), torch.ones(2, device="cuda")
+    x = torch.ones_like(dy)        # h is 0 and 3
+    ds.ds_layernorm_backward(M, ds.make_matrix(x), mean, rstd, None, ds.DS_F32, None, ds.make_matrix(torch.empty_like(dy)), dgamma, dbeta,
+                             ws.data_ptr(), need, stream())
+    assert torch.equal(dbeta, want) and torch.equal(dgamma, 3 * dy[1].float()) and whole()
