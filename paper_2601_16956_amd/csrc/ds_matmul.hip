@@ -43,10 +43,10 @@ __device__ inline f32x4 mfma(u32x4 x, u32x4 y, f32x4 sum, __half) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), sum, 0, 0, 0);
 }
 
-template <uint32_t ACT>
+template <uint32_t ACT, bool FULL>
 __device__ inline void activate8(Eight &z) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) z.v[k] = activation<ACT>(z.v[k]);
+  for (int k = 0; k < 8; ++k) z.v[k] = activation<ACT, FULL>(z.v[k]);
 }
 
 // The first n <= 8 of eight biases from column j on, zeros where there is none.
@@ -66,9 +66,9 @@ __device__ inline void finish8(const Epilogue &e, int64_t i, int64_t j, int n, E
     }
     mx8_put(e.saved, i, j, n, s);
   }
-  if (e.act == DS_ACT_GELU) activate8<DS_ACT_GELU>(z);
-  else if (e.act == DS_ACT_GELU_TANH) activate8<DS_ACT_GELU_TANH>(z);
-  else if (e.act == DS_ACT_SILU) activate8<DS_ACT_SILU>(z);
+  if (e.act == DS_ACT_GELU) activate8<DS_ACT_GELU, sizeof(T) == 4>(z);
+  else if (e.act == DS_ACT_GELU_TANH) activate8<DS_ACT_GELU_TANH, sizeof(T) == 4>(z);
+  else if (e.act == DS_ACT_SILU) activate8<DS_ACT_SILU, sizeof(T) == 4>(z);
   if (n <= 0) return;
   if (e.residual.base) {
     const Eight r = RowsOf<T>::value(residual, 8);

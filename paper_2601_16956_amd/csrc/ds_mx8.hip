@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kThreads) void ds_activation_backward_kernel(Rows d
     Eight r;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      r.v[k] = d.v[k] * activation_slope<ACT>(at.v[k]);
+      r.v[k] = d.v[k] * activation_slope<ACT, sizeof(T) == 4>(at.v[k]);
       sum.v[k] += k < n ? r.v[k] : 0.f;
     }
     put_up_to8<T>(dz.base, i * dz.stride + j, n, r);
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(1024) void ds_activation_backward_few_kernel(Rows d
     Eight r;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      r.v[k] = g.v[k] * activation_slope<ACT>(x.v[k]);
+      r.v[k] = g.v[k] * activation_slope<ACT, sizeof(T) == 4>(x.v[k]);
       sum.v[k] += k < n ? r.v[k] : 0.f;
     }
     put_up_to8<T>(dz.base, i * dz.stride + j, n, r);

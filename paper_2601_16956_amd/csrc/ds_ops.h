@@ -342,33 +342,79 @@ __device__ inline void mx8_put(const Rows &m, int64_t i, int64_t j, int n, const
 
 // ---- device: activations ---------------------------------------------------------------------------------------
 
-// 1 / (1 + exp(-x)): exp overflows to infinity for very negative x, and the quotient is then 0, its limit.
-// v_rcp_f32 is off by one unit of the last place at most, a division in full takes ten instructions more.
-__device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
+// FULL: for results of 32 bits, every factor to a few units of the last place, out to where results are subnormal.  Else, for results
+// that are rounded to 16 bits, the exponential is v_exp_f32 of a rounded product, off by up to |argument| * 2^-24 of itself (4e-6 at
+// -80), and the reciprocal v_rcp_f32, off by one unit: far below the rounding that follows.  (What FULL costs, f32: the backward
+// pass of 8192 x 3584 0 to 1 %, a product 8192 x 1024 x 8192 with GELU 195 and 197 us, with its tanh form 177 and 184.)
+
+// 1 / x for 1 <= x <= 8, to a unit of the last place: a step of Newton's behind the approximation.
+__device__ inline float reciprocal(float x) {
+  const float r = __builtin_amdgcn_rcpf(x);
+  return __builtin_fmaf(__builtin_fmaf(-x, r, 1.f), r, r);
+}
+// p = 1 / (1 + exp(-x)), and q = 1 - p without the cancellation.
+template <bool FULL>
+__device__ inline float sigmoid(float x, float &q) {
+  if (FULL) {  // exp of what is not positive cannot overflow
+    const float e = expf(-__builtin_fabsf(x)), high = reciprocal(1.f + e), low = e * high;
+    q = x < 0.f ? high : low;
+    return x < 0.f ? low : high;
+  }
+  // exp overflows to infinity for very negative x, and the reciprocal is then 0, its limit (below 2^-126 so too)
+  const float p = __builtin_amdgcn_rcpf(1.f + __expf(-x));
+  q = 1.f - p;
+  return p;
+}
+// The part of the normal distribution below z, and gauss = exp(-z^2 / 2).  Below -w it is gauss * t P(t), t = 1 / (1 + 0.35 w), P the
+// polynomial of eight degrees whose largest error of itself over 0 <= w <= 20 is least: 4.4e-8 (a weighted least-squares
+// fit to exp(w^2 / 2) erfc(w / sqrt(2)) / 2).  In units of itself: 1 + erf loses its digits where z is negative, all of
+// them from -5.5 on.  Beyond 20 nothing is left in 32 bits.
+template <bool FULL>
+__device__ inline float normal_below(float z, float &gauss) {
+  const float far = __builtin_fabsf(z), w = far > 20.f ? 20.f : far, square = w * w;
+  if (FULL) {
+    gauss = expf(-0.5f * square);
+    gauss = __builtin_fmaf(-0.5f * __builtin_fmaf(w, w, -square), gauss, gauss);  // what the square's rounding left out
+  } else {
+    gauss = __expf(-0.5f * square);
+  }
+  const float t = FULL ? reciprocal(__builtin_fmaf(0.35f, w, 1.f)) : __builtin_amdgcn_rcpf(__builtin_fmaf(0.35f, w, 1.f));
+  constexpr float P[9] = {0.139622584f, 0.139836043f, 0.120061718f, 0.104427479f, -0.0201176777f, 0.154166251f, -0.250737578f, 0.141272306f, -0.0285311043f};
+  float sum = P[8];
+#pragma unroll
+  for (int k = 7; k >= 0; --k) sum = __builtin_fmaf(sum, t, P[k]);
+  const float tail = gauss * (sum * t);
+  return z < 0.f ? tail : 1.f - tail;
+}
 constexpr float kGeluTanh = 0.7978845608028654f;  // sqrt(2 / pi)
 constexpr float kGeluCube = 0.044715f;
 
 // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)), so the tanh form is z * sigmoid(2 u).  At z = -infinity the products would be
 // infinity times 0; the limit is 0.
-template <uint32_t ACT>
+template <uint32_t ACT, bool FULL>
 __device__ inline float activation(float z) {
-  if (ACT == DS_ACT_GELU) return z == -__builtin_inff() ? 0.f : 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-  if (ACT == DS_ACT_GELU_TANH) return z == -__builtin_inff() ? 0.f : z * sigmoid(2.f * kGeluTanh * (z + kGeluCube * z * z * z));
-  if (ACT == DS_ACT_SILU) return z == -__builtin_inff() ? 0.f : z * sigmoid(z);
+  float other;
+  if (ACT == DS_ACT_GELU) return z == -__builtin_inff() ? 0.f : z * normal_below<FULL>(z, other);
+  if (ACT == DS_ACT_GELU_TANH) return z == -__builtin_inff() ? 0.f : z * sigmoid<FULL>(2.f * kGeluTanh * (z + kGeluCube * z * z * z), other);
+  if (ACT == DS_ACT_SILU) return z == -__builtin_inff() ? 0.f : z * sigmoid<FULL>(z, other);
   return z;
 }
-template <uint32_t ACT>
+// (Where gauss or p q is 0, z may be infinite.)
+template <uint32_t ACT, bool FULL>
 __device__ inline float activation_slope(float z) {
   if (ACT == DS_ACT_GELU) {
-    const float gauss = __expf(-0.5f * z * z);  // 0 where z is so large that z * gauss would be infinity times 0
-    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + (gauss == 0.f ? 0.f : z * gauss * 0.3989422804014327f);
+    float gauss;
+    const float p = normal_below<FULL>(z, gauss);
+    return p + (gauss == 0.f ? 0.f : z * gauss * 0.3989422804014327f);
   }
   if (ACT == DS_ACT_GELU_TANH) {
-    const float p = sigmoid(2.f * kGeluTanh * (z + kGeluCube * z * z * z)), flat = p * (1.f - p);
+    float q;
+    const float p = sigmoid<FULL>(2.f * kGeluTanh * (z + kGeluCube * z * z * z), q), flat = p * q;
     return p + (flat == 0.f ? 0.f : z * flat * 2.f * kGeluTanh * (1.f + 3.f * kGeluCube * z * z));
   }
   if (ACT == DS_ACT_SILU) {
-    const float p = sigmoid(z), flat = p * (1.f - p);
+    float q;
+    const float p = sigmoid<FULL>(z, q), flat = p * q;
     return p + (flat == 0.f ? 0.f : z * flat);
   }
   return 1.f;
