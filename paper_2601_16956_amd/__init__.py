@@ -171,14 +171,21 @@ def hip_runtime_in_use() -> List[str]:
         return []
 
 
-def kernel_source_digest() -> str:
-    """SHA-256 (first 16 hex digits) over the kernel sources and the compiler's flags; a counter profile names the digest it was
-    taken with, so that a reader of a measurement can tell whether the profile still describes the kernels in use."""
+_KERNEL_SOURCES = {
+    "capture": ("ds_kernels.hip", "ds_blocks.h", "ds_splice.h", "ds_internal.h", "ds_perm.h"),
+    "operators": ("ds_ops.h", "ds_internal.h", "ds_mx8.hip", "ds_norm.hip", "ds_choice.h", "ds_matmul.hip"),
+}
+
+
+def kernel_source_digest(of: str = "capture") -> str:
+    """SHA-256 (first 16 hex digits) over the kernel sources of the capture, or of the training step's "operators", and the
+    compiler's flags; a profile names the digest it was taken with, so that a reader of a measurement can tell whether the profile still
+    describes the kernels in use."""
     import hashlib
 
     from .build import HIPCC_FLAGS
     h = hashlib.sha256("\0".join(HIPCC_FLAGS).encode())
-    for name in ("ds_kernels.hip", "ds_blocks.h", "ds_splice.h", "ds_internal.h", "ds_perm.h"):
+    for name in _KERNEL_SOURCES[of]:
         with open(os.path.join(_HERE, "csrc", name), "rb") as f:
             h.update(f.read())
     return h.hexdigest()[:16]

@@ -162,3 +162,21 @@ def test_no_inline_assembly_writes_m0():
                 assert '"{m0}"(' in code, (name, code)
                 uses += 1
     assert uses >= 1
+
+
+def test_every_kernel_source_is_in_a_digest(tmp_path, monkeypatch):
+    import shutil
+
+    import paper_2601_16956_amd as ds
+    shutil.copytree(os.path.join(ROOT, "paper_2601_16956_amd", "csrc"), tmp_path / "csrc")
+    before = {of: ds.kernel_source_digest(of) for of in ("capture", "operators")}
+    assert ds.kernel_source_digest() == before["capture"] != before["operators"]
+    monkeypatch.setattr(ds, "_HERE", str(tmp_path))
+    assert {of: ds.kernel_source_digest(of) for of in before} == before
+    for name in sorted(os.listdir(tmp_path / "csrc")):
+        if name.endswith((".hip", ".h")):
+            path = tmp_path / "csrc" / name
+            text = path.read_bytes()
+            path.write_bytes(text + b"\n")
+            assert any(ds.kernel_source_digest(of) != d for of, d in before.items()), name
+            path.write_bytes(text)
