@@ -76,12 +76,27 @@ inline uint64_t lines_bytes(const Operand &o, int64_t depth) {
   return ((uint64_t)lines * (uint64_t)((length + 7) / 8 * 8) * 2 + 127) / 128 * 128;
 }
 
+// At most 16 rows on lines along k: does the kernel for them take the product, or the tiles?  It reads b once and joins nothing, but each of
+// its work-groups walks along all of k, and with n <= 2048 there are few of them; tiles split k.  And where k is short and n long
+// its work-groups, one a CU, come in several rounds.  us of the GPU, it / tiles, bfloat16, 1 and 16 rows:
+//      k     n = 64      n = 1024     n = 2048     n = 4096     n = 8192    n = 16384    n = 28672
+//    512   7.1/14  4/6   4.2/6  5/6   4.0/6  4/6   4.3/7  5/7   5.9/7  7/7   7.8/7  8/7   13/9  14/10
+//   4096   7.5/10 10/9   8.0/10 11/10 8.1/11 11/12 8.9/13 11/13 17/19 23/20  31/39 33/40  52/52 58/54
+//   8192    12/11 17/10   12/11 18/12  13/13 18/14  17/20 22/21 30/39 40/41  63/66 64/68  109/104 115/104
+//  16384    21/13 31/12   22/14 32/15  23/22 33/23  32/65 37/67 60/115 68/111 108/179 101/174 195/199 191/199
+// (Elsewhere, n = 6144 and 12288 with k >= 4096, either is up to 25 % ahead; this kernel has them.)
+inline bool few_rows(int64_t m, int64_t n, int64_t depth) {
+  if (m > kFewRows || n > kMaxTiles * 32) return false;
+  if (n <= 2048) return depth <= 7000 - 200 * m + 2 * (n > 1024 ? n - 1024 : 0);
+  return n <= 8192 || depth >= 1024;
+}
+
 inline Choice choose(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t depth) {
   Choice c{tiles_of(m, n, 64, 64) <= kMaxTiles ? Way::kSimple : Way::kNone, 0, 1, false, false, 0, 0, 0, 0};
   // lines of 16-bit values are at most 2^22 bytes apart, so that a stage's offsets have 31 bits
   const auto too_long = [&](const Operand &o) { return (o.k_last ? depth : o.extent) > (1 << 21); };
   if (depth == 0) return c;
-  if (m <= kFewRows && a.k_last && b.k_last && !a.scale && !b.scale && n <= kMaxTiles * 32) {
+  if (a.k_last && b.k_last && !a.scale && !b.scale && few_rows(m, n, depth)) {
     c.way = Way::kFew;
     return c;
   }

@@ -7,7 +7,7 @@
 //             the matrix cores and, at the largest sizes, by the power that they draw: 16384 x 3584 x 8192 in bfloat16
 //             708 us, 1.36 PFLOP/s (a library's product 716 to 728), with a residual 770; 8192^3 750 to 820 us.
 //             Zeros instead of normal numbers run a fifth faster.
-//   few rows  at most 16 rows on a weight [out, in]: bound by reading the weight, 1 x 8192 x 3584 in 13 us, 4.5 TB/s.
+//   few rows  at most 16 rows on a weight [out, in], save where n is small and k long: bound by reading the weight, 1 x 8192 x 3584 in 13 us, 4.5 TB/s.
 //   simple    whatever is left: products of less than 2^18 multiplications, and lines beyond 2^21 elements.
 //
 // Always: 32-bit sums; v_mfma_f32_16x16x32 with the operands exchanged, so that a lane's four results are neighbouring

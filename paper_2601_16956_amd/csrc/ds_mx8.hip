@@ -133,9 +133,9 @@ __global__ __launch_bounds__(kThreads) void ds_sum_parts_kernel(const float *par
 }
 
 // Few rows: a work-group has 64 columns, eight lanes a row of them and 128 rows at a time, and sums the bias's gradient itself: one launch.
-// So / by the kernel above and the sum of its lines, us of the GPU, silu on bfloat16 from 8 bits: 1 x 1024 4.0 / 4.9, 64 x 16384 4.6 / 6.3,
-// 128 x 1024 4.6 / 5.3, 333 x 1024 5.8 / 5.8, 512 x 1024 7.2 / 5.7; a caller who does not wait in between, 333 x 1024, 10.8 /
-// 14.2.
+// So / by the kernel above and the sum of its lines, us of the GPU, silu on bfloat16 from 8 bits: 1 x 1024 3.8 / 5.1, 128 x 1024 4.4 / 5.6, 256 x
+// 1024 5.3 / 5.5, 333 x 1024 6.3 / 6.1, 384 x 1024 6.8 / 6.3 and 512 x 1024 7.2 / 5.7; 384 x 256 6.1 / 6.1, 384 x 4096 7.3 / 8.3, 1 x 16384
+// 4.1 / 5.5, 384 x 16384 10.9 / 14.5.  A caller who does not wait in between has a launch less: 333 x 1024 10.8 / 14.2.
 constexpr int64_t kFewRows = 384, kFewCols = 16384;
 template <typename T, typename Z, uint32_t ACT>
 __global__ __launch_bounds__(1024) void ds_activation_backward_few_kernel(Rows dy, Rows z, Rows dz, int rows, int64_t cols, float *dbias) {

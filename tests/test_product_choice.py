@@ -70,6 +70,11 @@ def test_the_workspace_is_what_the_choice_needs(choose):
 def test_few_rows_and_small_products_have_ways_of_their_own(choose):
     assert choose(*matrices(1, 8192, 3584))["way"] == choose(*matrices(16, 100, 33))["way"] == "few rows"
     assert choose(*matrices(17, 8192, 3584))["way"] == choose(*matrices(1, 8192, 3584, "nn"))["way"] == "tiles"
+    # at most 16 rows, but k so long beside n that its splits are the quicker way, or columns so many beside k
+    for m, k, n, way in ((1, 16384, 64, "tiles"), (16, 4096, 1024, "tiles"), (16, 16384, 2048, "tiles"), (1, 512, 16384, "tiles"), (16, 512, 8193, "tiles"),
+                         (1, 6800, 64, "few rows"), (16, 3800, 1024, "few rows"), (1, 16384, 4096, "few rows"), (16, 1024, 16384, "few rows"),
+                         (16, 64, 8192, "few rows"), (5, 4096, 64, "few rows")):
+        assert choose(*matrices(m, k, n))["way"] == way, (m, k, n)
     assert choose(*matrices(33, 100, 40))["way"] == choose(*matrices(70, 0, 40))["way"] == "simple"
 
 
@@ -98,6 +103,14 @@ def test_products_of_far_extents_fit_a_launch_or_are_refused_by_both(choose, siz
         (how["lines_a"], *((k, m) if layout[0] == "t" else (m, k))), (how["lines_b"], *((n, k) if layout[1] == "t" else (k, n)))) if out)
     partial = 4 * how["splits"] * m * n if how["splits"] > 1 else 0
     assert lines + partial <= how["bytes"] <= lines + partial + 256 and how["bytes"] == ds.ds_matmul_workspace(a, b, c)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,k,n", [(1, 20011, 4104), (16, 9000, 2100), (7, 1500, 9001), (1, 16384, 64), (16, 5000, 1000), (3, 700, 9100)])
+def test_few_rows_by_either_way(m, k, n):
+    import test_gpu_training_ops as ops
+    for kw in ({}, {"kind": "f16", "out": "f32", "act": "silu", "bias": "f16", "residual": True, "pad": 5, "shift": 1, "save": True}):
+        ops.product_case(m, k, n, layout="nt", **kw)
 
 
 @pytest.mark.gpu
