@@ -147,6 +147,10 @@ def main(argv=None):
     ap.add_argument("--ffn", type=int, default=1024)
     ap.add_argument("--dir", default=tempfile.gettempdir())
     a = ap.parse_args(argv)
+    if not 0 <= a.snapshot_at < a.steps:
+        ap.error("--snapshot-at names one of the steps, 0 to --steps - 1")
+    if min(a.rows, a.hidden, a.ffn) < 1:
+        ap.error("--rows, --hidden and --ffn are at least 1")
     block = Block(a.rows, a.hidden, a.ffn)
     tensors = block.state()
     descs = ds.make_descs_from_tensors(tensors)

@@ -310,3 +310,16 @@ def test_a_product_s_workspace_goes_by_strides_and_alignment():
     for a in (mat(m, k, base=PTR + 2), mat(m, k, row=k + 4), mat(m, k, ds.DS_MX8)):
         assert ds.ds_matmul_workspace(a, b, c) == m * k * 2
         assert product(a, b, c, ws=None, size=0) == ds.DS_EINVAL
+
+
+@pytest.mark.parametrize("args", (["--snapshot-at", "40"], ["--snapshot-at", "-1"], ["--steps", "0"], ["--rows", "0"], ["--ffn", "-3"]))
+def test_the_example_refuses_steps_that_it_does_not_take(args, capsys):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_mlp.py")
+    spec = importlib.util.spec_from_file_location("train_mlp_arguments", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    with pytest.raises(SystemExit) as e:
+        example.main(args)
+    assert e.value.code == 2 and "error: --" in capsys.readouterr().err
