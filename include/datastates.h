@@ -656,7 +656,12 @@ int ds_ckpt_restore_parts(const ds_ckpt_reader *const *readers, uint32_t n_parts
  * NaN: such a group reads as NaN.  A value is off by at most half a step of
  * 2^(E - 6), by less than one where it was limited, and is representable in the
  * type it came from, so that it is read back without another rounding.  Codes
- * and scales are bytes and can be captured as shards (DS_U8).
+ * and scales are bytes and can be captured as shards (DS_U8).  (The values are
+ * those of MXINT8 of the Open Compute Project's microscaling formats: 8-bit
+ * whole numbers of 2^-6 under an E8M0 byte for 32 of them, 255 for NaN.  Where
+ * that leaves a choice: the code -128 is read but never written, a group of
+ * zeros has byte 0 and any other 1 at least, and a group without values has
+ * codes 0.)
  */
 typedef struct ds_matrix {
   void *base;

@@ -5,9 +5,10 @@
 //             passing registers, in either order of each; few tiles are split along k, and joined by a second launch.
 //             Operands that are no whole 16-byte pieces, or checkpoints in 8 bits, are laid out in the workspace first.  Bound by
 //             the matrix cores and, at the largest sizes, by the power that they draw: 16384 x 3584 x 8192 in bfloat16
-//             708 us, 1.36 PFLOP/s (a library's product 716 to 728), with a residual 770; 8192^3 750 to 820 us.
-//             Zeros instead of normal numbers run a fifth faster.
-//   few rows  at most 16 rows on a weight [out, in], save where n is small and k long: bound by reading the weight, 1 x 8192 x 3584 in 13 us, 4.5 TB/s.
+//             712 to 724 us, 1.33 to 1.35 PFLOP/s, with a residual 765 to 769 (a library's product 626 to 728 us, as data and card let it); 8192^3
+//             770 to 802 us (690 to 796).  Zeros instead of normal numbers run a fifth faster.
+//   few rows  at most 16 rows on a weight [out, in], save where n is small and k long: bound by reading
+//             the weight, 1 x 8192 x 3584 in 15 us, 3.9 TB/s.
 //   simple    whatever is left: products of less than 2^18 multiplications, and lines beyond 2^21 elements.
 //
 // Always: 32-bit sums; v_mfma_f32_16x16x32 with the operands exchanged, so that a lane's four results are neighbouring
@@ -223,8 +224,8 @@ __device__ inline void stage_is_there() {
 // The part of one operand that a work-group stages: P lines or columns, kStep of k.
 //   K_LAST: LDS holds P rows of 128 bytes, eight pieces of eight k; piece c of row r is at c ^ (r % 8).  A read takes 16 lanes
 //     at a time, lanes 0-3, 12-15 and 20-27 first: rows 0-3 and 12-15 at one c and rows 4-11 at the next, which then lie in
-//     different banks.  (Rows of 64 bytes, so that a stage is half as deep, make twice the requests of the L2: 8192^3 in
-//     876 us, 958 so.)
+//     different banks.  (Rows of 64 bytes, so that a stage is half as deep, make twice the requests of the L2: 8192^3
+//     took a tenth longer so, 958 us against 876 in the loop of the time.)
 //   else: LDS holds kStep rows of P elements.  A lane's eight k are then in eight rows: ds_read_b64_tr_b16 reads four rows of 16
 //     elements with 16 lanes and gives each lane one column of them.  Pairs of pieces are exchanged by the row, so that
 //     the 32 lanes of a pass, eight rows of 32 bytes, meet every bank once.

@@ -9,7 +9,7 @@
 // every pass, out of the caches.
 //
 // 8192 rows of 4096 bfloat16: forward with a checkpoint in 8 bits 34 us (168 MB, 4.9 TB/s), backward from it with a residual 49 us (236
-// MB, 4.8 TB/s) and 5 us for the lines.  One row of 8192: 4 us, the chain of its loads, two sums over 16 wavefronts and the store.
+// MB, 4.8 TB/s) and 6 us for the lines.  One row of 8192: 4 us, the chain of its loads, two sums over 16 wavefronts and the store.
 
 #include <type_traits>
 
@@ -336,8 +336,8 @@ __global__ __launch_bounds__(256) void ds_layernorm_params_long_kernel(NormBackw
   }
 }
 
-// Rows of so many columns fit the registers of a work-group with two pieces a thread: forward of 16 wavefronts, backward of 8 (16
-// would have 128 registers each).
+// Rows of so many columns fit the registers of a work-group with two pieces a thread: forward of 16 wavefronts, backward of 8 (with two
+// pieces a thread has about 200 registers, and 16 wavefronts leave each thread 128; one piece on 16 is not tried).
 constexpr int64_t kLongest = 16384, kLongestBackward = 8192;
 
 // Work-groups: as many as run at once, or one for each set of rows.  (Backward each is a line that is written and read again.)
