@@ -43,7 +43,8 @@ struct Choice {
 };
 // A tile's extents, how many of its work-groups a CU holds, and what they take, in us: before and behind the steps; a step where most
 // CUs are idle; a step with 1, 2, 3 work-groups on every CU.  (Measured with bfloat16 [out, in] on products of 4 to 256 steps; what
-// the steps take on a full chip is decided by its power.)
+// the steps take on a full chip is decided by its power.  Neither the epilogue is in them, nor laying out lines, nor memory that cannot
+// follow: 515 x 1000 x 777 is put at 9 us and takes 12, and 4 for the lines.)
 struct TileSize {
   int m, n, at_once;
   double around, idle, step[3];

@@ -5,8 +5,8 @@
 //             passing registers, in either order of each; few tiles are split along k, and joined by a second launch.
 //             Operands that are no whole 16-byte pieces, or checkpoints in 8 bits, are laid out in the workspace first.  Bound by
 //             the matrix cores and, at the largest sizes, by the power that they draw: 16384 x 3584 x 8192 in bfloat16
-//             712 to 724 us, 1.33 to 1.35 PFLOP/s, with a residual 765 to 769 (a library's product 626 to 728 us, as data and card let it); 8192^3
-//             770 to 802 us (690 to 796).  Zeros instead of normal numbers run a fifth faster.
+//             about 720 us, 1.34 PFLOP/s, with a residual 770 (a library's product 626 to 728 us, as data and card let it);
+//             8192^3 about 790 us (690 to 796).  Zeros instead of normal numbers run a fifth faster.
 //   few rows  at most 16 rows on a weight [out, in], save where n is small and k long: bound by reading
 //             the weight, 1 x 8192 x 3584 in 15 us, 3.9 TB/s.
 //   simple    whatever is left: products of less than 2^18 multiplications, and lines beyond 2^21 elements.
