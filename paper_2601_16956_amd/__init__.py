@@ -778,7 +778,7 @@ def make_mx8(codes, scale) -> ds_matrix:
 def _vector(v, dtype: int, matrix: ds_matrix, axis: str, what: str):
     """The address of a vector: an address as it is (nothing is known of it, so nothing is checked), or that of a 1-D
     contiguous torch tensor on the GPU with an element of `dtype` for each of the matrix's rows or cols."""
-    if v is None or type(v) is int or not hasattr(v, "data_ptr"):
+    if v is None or not hasattr(v, "data_ptr"):
         return v
     length = getattr(matrix, axis)
     if _float_code(v.dtype) != dtype:
@@ -823,8 +823,9 @@ def ds_mx8_load(saved: ds_matrix, x: ds_matrix, stream: int = 0) -> None:
 
 def ds_layernorm_forward(x: ds_matrix, gamma, beta, param_dtype: int, eps: float, y: ds_matrix, mean=None, rstd=None,
                          saved: Optional[ds_matrix] = None, stream: int = 0) -> None:
-    gamma, beta = _vector(gamma, param_dtype, x, "cols", "gamma"), _vector(beta, param_dtype, x, "cols", "beta")
-    mean, rstd = _vector(mean, DS_F32, x, "rows", "mean"), _vector(rstd, DS_F32, x, "rows", "rstd")
+    if not (type(gamma) is type(beta) is type(mean) is type(rstd) is int):
+        gamma, beta = _vector(gamma, param_dtype, x, "cols", "gamma"), _vector(beta, param_dtype, x, "cols", "beta")
+        mean, rstd = _vector(mean, DS_F32, x, "rows", "mean"), _vector(rstd, DS_F32, x, "rows", "rstd")
     _check(_lib.ds_layernorm_forward(x, gamma, beta, param_dtype, eps, y, mean, rstd, saved, stream), "ds_layernorm_forward")
 
 
@@ -836,9 +837,10 @@ def ds_layernorm_backward_workspace(rows: int, cols: int) -> int:
 
 def ds_layernorm_backward(dy: ds_matrix, x: ds_matrix, mean, rstd, gamma, param_dtype: int, residual: Optional[ds_matrix],
                           dx: ds_matrix, dgamma, dbeta, workspace: Optional[int], workspace_bytes: int, stream: int = 0) -> None:
-    mean, rstd = _vector(mean, DS_F32, dy, "rows", "mean"), _vector(rstd, DS_F32, dy, "rows", "rstd")
-    gamma = _vector(gamma, param_dtype, dy, "cols", "gamma")
-    dgamma, dbeta = _vector(dgamma, DS_F32, dy, "cols", "dgamma"), _vector(dbeta, DS_F32, dy, "cols", "dbeta")
+    if not (type(mean) is type(rstd) is type(gamma) is type(dgamma) is type(dbeta) is int):
+        mean, rstd = _vector(mean, DS_F32, dy, "rows", "mean"), _vector(rstd, DS_F32, dy, "rows", "rstd")
+        gamma = _vector(gamma, param_dtype, dy, "cols", "gamma")
+        dgamma, dbeta = _vector(dgamma, DS_F32, dy, "cols", "dgamma"), _vector(dbeta, DS_F32, dy, "cols", "dbeta")
     _check(_lib.ds_layernorm_backward(dy, x, mean, rstd, gamma, param_dtype, residual, dx, dgamma, dbeta, workspace,
                                       workspace_bytes, stream), "ds_layernorm_backward")
 
@@ -852,10 +854,10 @@ def ds_matmul_workspace(a: ds_matrix, b: ds_matrix, c: ds_matrix) -> int:
 
 def ds_matmul(a: ds_matrix, b: ds_matrix, c: ds_matrix, epilogue: Optional[ds_matmul_epilogue] = None,
               workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
-    if epilogue is not None and epilogue.bias_length:
-        address, length = epilogue.bias_length
-        if address == epilogue.bias and length < b.cols:
-            raise ValueError(f"the bias has {length} elements for {b.cols} columns")
+    if epilogue is not None:
+        known = epilogue.bias_length
+        if known is not None and known[1] < b.cols and known[0] == epilogue.bias:
+            raise ValueError(f"the bias has {known[1]} elements for {b.cols} columns")
     _check(_lib.ds_matmul(a, b, c, epilogue, workspace, workspace_bytes, stream), "ds_matmul")
 
 
@@ -867,5 +869,6 @@ def ds_activation_backward_workspace(rows: int, cols: int) -> int:
 
 def ds_activation_backward(dy: ds_matrix, z: ds_matrix, act: int, dz: ds_matrix, dbias, workspace: Optional[int] = None,
                            workspace_bytes: int = 0, stream: int = 0) -> None:
-    dbias = _vector(dbias, DS_F32, dy, "cols", "dbias")
+    if type(dbias) is not int:
+        dbias = _vector(dbias, DS_F32, dy, "cols", "dbias")
     _check(_lib.ds_activation_backward(dy, z, act, dz, dbias, workspace, workspace_bytes, stream), "ds_activation_backward")

@@ -56,8 +56,8 @@ constexpr TileSize kTiles[] = {
 };
 constexpr int64_t kCus = 256;
 inline int64_t tiles_of(int64_t m, int64_t n, int64_t tile_m, int64_t tile_n) { return (m + tile_m - 1) / tile_m * ((n + tile_n - 1) / tile_n); }
-inline double tile_time(const TileSize &s, int64_t m, int64_t n, int64_t steps, int64_t splits) {
-  const int64_t groups = tiles_of(m, n, s.m, s.n) * splits, each = (steps + splits - 1) / splits;
+inline double tile_time(const TileSize &s, int64_t tiles, int64_t m, int64_t n, int64_t steps, int64_t splits) {
+  const int64_t groups = tiles * splits, each = (steps + splits - 1) / splits;
   const int64_t on_cu = (groups + kCus - 1) / kCus, rounds = (on_cu + s.at_once - 1) / s.at_once, rest = on_cu % s.at_once;
   double step = (double)(on_cu / s.at_once) * s.step[s.at_once - 1] + (rest ? s.step[rest - 1] : 0.0);
   if (on_cu == 1) step = s.idle + (s.step[0] - s.idle) * (double)groups / kCus;
@@ -104,12 +104,13 @@ inline Choice choose(const Operand &a, const Operand &b, int64_t m, int64_t n, i
   if ((double)m * (double)n * (double)depth < (1 << 18) || too_long(a) || too_long(b)) return c;
   const int64_t steps = (depth + kStep - 1) / kStep;
   double best = 1e300;
-  for (int i = 0; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i)
-    for (int64_t splits = 1; splits <= 16 && splits * 4 <= steps + 3; ++splits) {
-      if (tiles_of(m, n, kTiles[i].m, kTiles[i].n) * splits > kMaxTiles) break;
-      const double time = tile_time(kTiles[i], m, n, steps, splits);
+  for (int i = 0; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i) {
+    const int64_t tiles = tiles_of(m, n, kTiles[i].m, kTiles[i].n);
+    for (int64_t splits = 1; splits <= 16 && splits * 4 <= steps + 3 && tiles * splits <= kMaxTiles; ++splits) {
+      const double time = tile_time(kTiles[i], tiles, m, n, steps, splits);
       if (time < best) best = time, c.way = Way::kTile, c.tile = i, c.splits = (uint32_t)splits;
     }
+  }
   if (c.way != Way::kTile) return c;
   c.lines_a = !in_pieces(a, depth), c.lines_b = !in_pieces(b, depth);
   if (c.lines_a) c.at_a = c.bytes, c.bytes += lines_bytes(a, depth);
