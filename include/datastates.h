@@ -617,8 +617,10 @@ int ds_ckpt_restore_parts(const ds_ckpt_reader *const *readers, uint32_t n_parts
  * Operators of the forward and backward pass that runs while a snapshot drains:
  * checkpoints of activations in 8 bits, which leave HBM to the staging that
  * opens the gate early, and the layer norms, products and activations that
- * write and read them.  They only read the weights, so they may run before the
- * gate of the snapshot in flight (ds_event_wait_on_stream).
+ * write and read them; what joins blocks to the residual stream, the loss's log
+ * probabilities, and the update.  All but the update (ds_adamw_step) only read
+ * the state, so they may run before the gate of the snapshot in flight
+ * (ds_event_wait_on_stream).
  *
  *   - All are asynchronous on `stream`, allocate nothing, keep nothing between
  *     calls and may be captured into a graph.  A workspace is device memory of
@@ -638,6 +640,7 @@ int ds_ckpt_restore_parts(const ds_ckpt_reader *const *readers, uint32_t n_parts
  */
 
 #define DS_MX8 16u /* ds_matrix only: a checkpoint in 8 bits (below); not a type of shards */
+#define DS_UF8 17u /* ds_matrix only, where a function names it: values that are not negative in 8 bits (below) */
 
 /*
  * A matrix in device memory.  Element (i, j) is at base + itemsize *
@@ -662,6 +665,15 @@ int ds_ckpt_restore_parts(const ds_ckpt_reader *const *readers, uint32_t n_parts
  * that leaves a choice: the code -128 is read but never written, a group of
  * zeros has byte 0 and any other 1 at least, and a group without values has
  * codes 0.)
+ *
+ * DS_UF8, for values from 0 on that differ by many powers of two (second
+ * moments): laid out as DS_MX8 is, with unsigned codes.  Code c under byte s is the
+ * 32-bit float whose bits are (c + 8 s) << 20 -- five bits of exponent and three
+ * of fraction above 2^(s - 127) -- and 0 for c = 0.  s = max(0, F - 30), F the
+ * exponent field (value 2^(F - 127)) of the group's largest value; a value is
+ * rounded to the nearest code (ties to even), to 1 at least if it is not 0, and
+ * to the largest finite float at most.  The byte is 255, the codes 0 and the
+ * values NaN where any of the group is negative, infinite or NaN.
  */
 typedef struct ds_matrix {
   void *base;
@@ -669,13 +681,13 @@ typedef struct ds_matrix {
   uint32_t reserved; /* 0 */
   int64_t rows, cols;
   int64_t row_stride, col_stride; /* elements */
-  uint8_t *scale;                 /* DS_MX8, else NULL */
-  int64_t scale_stride;           /* DS_MX8: bytes from row to row, >= ceil(cols / 32); else 0 */
+  uint8_t *scale;                 /* DS_MX8 and DS_UF8, else NULL */
+  int64_t scale_stride;           /* DS_MX8 and DS_UF8: bytes from row to row, >= ceil(cols / 32); else 0 */
 } ds_matrix;
 
-/* x (DS_F32, DS_BF16, DS_F16; ROWS) into the checkpoint `saved` of the same
- * extents, and back: x is each value of `saved`, rounded where its type does not
- * hold it.  Errors: DS_EINVAL, DS_ERANGE, DS_EHIP. */
+/* x (DS_F32, DS_BF16, DS_F16; ROWS) into the checkpoint `saved` (DS_MX8 or DS_UF8) of
+ * the same extents, and back: x is each value of `saved`, rounded where its type
+ * does not hold it.  Errors: DS_EINVAL, DS_ERANGE, DS_EHIP. */
 int ds_mx8_save(const ds_matrix *x, const ds_matrix *saved, void *stream);
 int ds_mx8_load(const ds_matrix *saved, const ds_matrix *x, void *stream);
 
@@ -753,6 +765,167 @@ int ds_matmul(const ds_matrix *a, const ds_matrix *b, const ds_matrix *c, const 
 int ds_activation_backward_workspace(int64_t rows, int64_t cols, uint64_t *bytes);
 int ds_activation_backward(const ds_matrix *dy, const ds_matrix *z, uint32_t act, const ds_matrix *dz, float *dbias,
                            void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * A block's output u joined to the residual stream x, with what models put around
+ * that: a norm behind the block, its gate, the scale of the residual, and the
+ * norm in front of the next block.  Norms are by the root of the mean square.
+ *   v   = u * rstd_after * after_gamma      (DS_JOIN_AFTER; else v = u),
+ *         rstd_after  = 1 / sqrt(sum_j u_j^2 / cols + eps)
+ *   out = keep * x + scale * gate * v
+ *   y   = out * rstd_before * before_gamma  (DS_JOIN_BEFORE),
+ *         rstd_before = 1 / sqrt(sum_j out_j^2 / cols + eps)
+ * where out counts as it is stored, rounded to its type: the gradient has
+ * nothing else to start from.
+ */
+#define DS_JOIN_AFTER 1u
+#define DS_JOIN_BEFORE 2u
+typedef struct ds_join {
+  const void *after_gamma;  /* cols elements of param_dtype in device memory, or NULL (1); so are the next two */
+  const void *gate;
+  const void *before_gamma;
+  uint32_t param_dtype;     /* DS_F32, DS_BF16 or DS_F16 */
+  uint32_t norms;           /* DS_JOIN_*                 */
+  float keep, scale;
+  float eps;                /* >= 0 */
+  uint32_t reserved;        /* 0 */
+} ds_join;
+
+/*
+ * u, x, out, y: DS_F32, DS_BF16 or DS_F16, the same for all, ROWS, the same
+ * extents.  u: NULL in front of the first block; then out = x, which `out` = NULL
+ * says too, and neither `keep` nor what belongs to u counts.  y: NULL without
+ * DS_JOIN_BEFORE.  rstd_after, rstd_before: one float per row, each may be NULL.
+ * out may be x, and y may be u.  A row with a NaN or an infinity affects no
+ * other row.  A gamma or gate that its norm or u would use is NULL where there
+ * is no such norm or u.  Errors: DS_EINVAL, DS_ERANGE, DS_EHIP.
+ */
+int ds_join_forward(const ds_join *join, const ds_matrix *u, const ds_matrix *x, const ds_matrix *out, const ds_matrix *y,
+                    float *rstd_after, float *rstd_before, void *stream);
+
+/*
+ * Its gradient.  dout: what reaches out past the next norm, or NULL (0); dy: what
+ * reaches y, NULL without DS_JOIN_BEFORE.  With h = out * rstd_before, g = dy *
+ * before_gamma, k = u * rstd_after (u without that norm):
+ *   d  = dout + rstd_before * (g - h * sum_j g_j h_j / cols),  dx = keep * d,
+ *   dv = scale * gate * d, and with w = dv * after_gamma
+ *   du = rstd_after * (w - k * sum_j w_j k_j / cols)           (dv without the norm),
+ *   dbefore_j = sum over rows of dy * h,
+ *   dgate_j = sum of scale * d * k * after_gamma, dafter_j = sum of scale * gate * d * k.
+ * u, out: as the forward pass had and left them; rstd_*: what it left, NULL without
+ * their norm.  All matrices are of one type and extent, ROWS.  Without u (NULL)
+ * du, dgate and dafter are NULL and dx = d.  dx, du and the sums (cols floats,
+ * overwritten, with zeros where there are no rows) may each be NULL.  dx may be
+ * dout, du may be dy or u.  Errors: DS_EINVAL, DS_ERANGE, DS_EHIP.
+ */
+int ds_join_backward_workspace(int64_t rows, int64_t cols, uint64_t *bytes);
+int ds_join_backward(const ds_join *join, const ds_matrix *dout, const ds_matrix *dy, const ds_matrix *u, const ds_matrix *out,
+                     const float *rstd_after, const float *rstd_before, const ds_matrix *du, const ds_matrix *dx,
+                     float *dafter, float *dgate, float *dbefore, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Log probabilities of given tokens.  With z = scale * x over a row of the logits
+ * x (DS_F32, DS_BF16, DS_F16; ROWS), scale > 0 and finite (1 / temperature):
+ *   largest = max_j x_j,  logsum = log(sum_j exp(z_j - scale * largest)),
+ *   logp_j = z_j - scale * largest - logsum,  logprob = logp[token],
+ *   entropy = -sum_j exp(logp_j) logp_j.
+ * (The two numbers hold the digits that their sum would lose, and rows that are
+ * cut over several GPUs are joined by them.)
+ *   - tokens: one per row in device memory; one below 0 or from cols on is none,
+ *     and its logprob is 0.  May be NULL if logprob is.
+ *   - logprob, largest, logsum, entropy: one float per row, each may be NULL.
+ *   - The likeliest: the `top` (0 to DS_TOP_MOST) columns with the largest logits in
+ *     that order, of equal ones the lowest column first: top_tokens[i * top + r]
+ *     and top_logprobs[i * top + r], each may be NULL.  Columns of -infinity are left
+ *     out; where fewer than `top` are left, the rest has token -1 and -infinity.
+ *   - -infinity masks a column.  A row that is masked whole has logprob, largest and
+ *     logsum -infinity and entropy 0.  A row with a NaN or +infinity has NaN in all
+ *     its floats (logprob 0 for a token that is none) and tokens -1.
+ * workspace: NULL where ds_logprobs_workspace says 0.
+ * Errors: DS_EINVAL, DS_ERANGE, DS_EHIP.
+ */
+#define DS_TOP_MOST 32u
+int ds_logprobs_workspace(const ds_matrix *logits, uint32_t top, uint64_t *bytes);
+int ds_logprobs(const ds_matrix *logits, float scale, const int64_t *tokens, float *logprob, float *largest, float *logsum,
+                float *entropy, uint32_t top, int64_t *top_tokens, float *top_logprobs, void *workspace,
+                uint64_t workspace_bytes, void *stream);
+
+/*
+ * Its gradient, with p_j = exp(logp_j):
+ *   dlogits_j = scale * (dlogprob * ([j = token] - p_j) - dentropy * p_j * (logp_j + entropy)).
+ * largest, logsum: the forward pass's.  dlogprob: one float per row, or NULL (0);
+ * tokens may then be NULL.  dentropy: likewise, and entropy (the forward pass's)
+ * is needed where it is given.  dlogits: type and extents of logits, ROWS; it may
+ * be logits itself.  Rows whose token is none (or dlogprob 0) and whose dentropy is 0, and rows
+ * that are masked whole, have zeros whatever is in them; masked columns have p = 0.
+ * Errors: DS_EINVAL, DS_ERANGE, DS_EHIP.
+ */
+int ds_logprobs_backward(const ds_matrix *logits, float scale, const int64_t *tokens, const float *largest,
+                         const float *logsum, const float *entropy, const float *dlogprob, const float *dentropy,
+                         const ds_matrix *dlogits, void *stream);
+
+/*
+ * The update, which the gate of the snapshot in flight stands in front of: AdamW
+ * over all tensors of a table at once.  With t the number of this step (from 1
+ * on), q = sqrt(squares) * grad_scale, and
+ *   c = grad_scale * (q > most_norm > 0 ? most_norm / q : 1):
+ *   g = c * grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   r = settings' rate * tensor's rate,
+ *   param -= r * decay * param + r / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * and copy = param, rounded to copy's type (from 32 bits, as param is to its own).
+ *
+ * Moments are both DS_F32, or m DS_MX8 and v DS_UF8.  The latter are rounded at
+ * random, without a bias, where DS_MX8 and DS_UF8 otherwise say to nearest (which would
+ * lose every change that is smaller than half a step): with the 16 low bits a
+ * and the 16 high bits b of the element's random number, the code of m is
+ * floor(m / step + (a + 1/2) / 2^16), the sum rounded to 32 bits and the code limited
+ * to +-127, and that of v is ((bits(v) + 16 b + 8) >> 20) - 8 s.  The random number of
+ * element (i, j) of tensor k is mix(i * cols + j + mix(k + mix(t + mix(lo(seed) ^
+ * mix(hi(seed)))))), lo and hi the halves of 32 bits of the seed, sums modulo 2^32 and
+ *   mix(x): x ^= x >> 16; x *= 0x9E3779B9; x ^= x >> 15; x *= 0xBB67AE85; x ^= x >> 16.
+ * What the step computes from m and v is not rounded before.
+ */
+typedef struct ds_adamw ds_adamw;
+typedef struct ds_adamw_tensor {
+  ds_matrix param; /* DS_F32, DS_BF16 or DS_F16; all matrices: ROWS, the same extents                */
+  ds_matrix grad;  /* DS_F32, DS_BF16 or DS_F16                                                      */
+  ds_matrix m, v;  /* both DS_F32, or DS_MX8 and DS_UF8                                              */
+  ds_matrix copy;  /* DS_F32, DS_BF16 or DS_F16; all of it 0: none (its dtype is then not looked at) */
+  float decay;     /* weight decay, >= 0                                                             */
+  float rate;      /* factor of the settings' rate, >= 0                                             */
+} ds_adamw_tensor;
+
+typedef struct ds_adamw_settings {
+  double rate, beta1, beta2, eps; /* rate, eps >= 0; 0 <= beta < 1                                       */
+  double grad_scale;              /* 1 / the scale of the loss; finite                                   */
+  double most_norm;               /* norm of all gradients that is not clipped; 0: no clipping           */
+  uint64_t seed;                  /* of the rounding of moments in 8 bits                                */
+  const int64_t *step;            /* device memory: t (below 1 counts as 1)                              */
+  const float *rate_now;          /* device memory: taken for `rate`; or NULL                            */
+  const double *squares;          /* device memory: sum of all gradients' squares, before grad_scale; NULL: not known.
+                                     Where it is infinite or NaN nothing is changed at all.  Needed for clipping */
+} ds_adamw_settings;
+
+/*
+ * Checks the tensors and puts their table on the current device, once for all
+ * steps; `tensors` may be freed afterwards.  Tensors without elements are
+ * allowed.  Memory that the step writes must not be written for two tensors or
+ * twice for one: tables where two matrices begin at one address, or
+ * contiguous ones overlap, are refused (DS_EOVERLAP); interleaved views are not checked.
+ * The table may be used from several threads; steps on the same tensors are ordered by
+ * the caller.  Errors: DS_EINVAL, DS_ERANGE, DS_EOVERLAP, DS_ENOMEM, DS_EHIP.
+ */
+int ds_adamw_create(const ds_adamw_tensor *tensors, size_t n, ds_adamw **out);
+/* As ds_plan_destroy: nothing that uses the table may still run. */
+int ds_adamw_destroy(ds_adamw *table);
+
+/* *squares (device memory) = the sum of the squares of all gradients, in 64 bits.  (Ranks that share
+ * a model add theirs before the step.)  Errors, here and below: DS_EINVAL, DS_ERANGE, DS_EHIP, and
+ * DS_ESTATE where the table's device is not the current one. */
+int ds_adamw_squares_workspace(const ds_adamw *table, uint64_t *bytes);
+int ds_adamw_squares(const ds_adamw *table, double *squares, void *workspace, uint64_t workspace_bytes, void *stream);
+/* The settings are read before the call returns; what they point to, when the step runs. */
+int ds_adamw_step(const ds_adamw *table, const ds_adamw_settings *settings, void *stream);
 
 /* ---- misc ---------------------------------------------------------------- */
 

@@ -22,7 +22,9 @@ DS_EINVAL, DS_EALIGN, DS_EOVERLAP, DS_EGAP, DS_ERANGE, DS_ENOMEM, DS_EHIP, DS_EB
 DS_EFORMAT = -11
 DS_EFAULT = -12
 DS_ETOOBIG = -13
-DS_MX8 = 16  # ds_matrix only
+DS_MX8, DS_UF8 = 16, 17  # ds_matrix only
+DS_JOIN_AFTER, DS_JOIN_BEFORE = 1, 2
+DS_TOP_MOST = 32
 DS_ACT_NONE, DS_ACT_GELU, DS_ACT_GELU_TANH, DS_ACT_SILU = 0, 1, 2, 3
 DS_PACK_NOALLOC_TABLE_BYTES = 4 << 20
 DS_FILE_DIRECT, DS_FILE_SYNC, DS_FILE_URING = 1, 2, 4
@@ -47,6 +49,9 @@ EXPORTS = [
     "ds_ckpt_restore_parts", "ds_ckpt_append_from",
     "ds_mx8_save", "ds_mx8_load", "ds_layernorm_forward", "ds_layernorm_backward_workspace", "ds_layernorm_backward",
     "ds_matmul_workspace", "ds_matmul", "ds_activation_backward_workspace", "ds_activation_backward",
+    "ds_join_forward", "ds_join_backward_workspace", "ds_join_backward",
+    "ds_logprobs_workspace", "ds_logprobs", "ds_logprobs_backward",
+    "ds_adamw_create", "ds_adamw_destroy", "ds_adamw_squares_workspace", "ds_adamw_squares", "ds_adamw_step",
 ]
 
 
@@ -151,6 +156,48 @@ class ds_matmul_epilogue(ctypes.Structure):
     ]
 
 
+class ds_join(ctypes.Structure):
+    vectors = ()  # (what, elements) of the tensors that make_join took the vectors from
+    _fields_ = [
+        ("after_gamma", ctypes.c_void_p),
+        ("gate", ctypes.c_void_p),
+        ("before_gamma", ctypes.c_void_p),
+        ("param_dtype", ctypes.c_uint32),
+        ("norms", ctypes.c_uint32),
+        ("keep", ctypes.c_float),
+        ("scale", ctypes.c_float),
+        ("eps", ctypes.c_float),
+        ("reserved", ctypes.c_uint32),
+    ]
+
+
+class ds_adamw_tensor(ctypes.Structure):
+    _fields_ = [
+        ("param", ds_matrix),
+        ("grad", ds_matrix),
+        ("m", ds_matrix),
+        ("v", ds_matrix),
+        ("copy", ds_matrix),
+        ("decay", ctypes.c_float),
+        ("rate", ctypes.c_float),
+    ]
+
+
+class ds_adamw_settings(ctypes.Structure):
+    _fields_ = [
+        ("rate", ctypes.c_double),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("grad_scale", ctypes.c_double),
+        ("most_norm", ctypes.c_double),
+        ("seed", ctypes.c_uint64),
+        ("step", ctypes.c_void_p),
+        ("rate_now", ctypes.c_void_p),
+        ("squares", ctypes.c_void_p),
+    ]
+
+
 class DsError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -173,7 +220,8 @@ def hip_runtime_in_use() -> List[str]:
 
 _KERNEL_SOURCES = {
     "capture": ("ds_kernels.hip", "ds_blocks.h", "ds_splice.h", "ds_internal.h", "ds_perm.h"),
-    "operators": ("ds_ops.h", "ds_internal.h", "ds_mx8.hip", "ds_norm.hip", "ds_choice.h", "ds_matmul.hip"),
+    "operators": ("ds_ops.h", "ds_internal.h", "ds_mx8.hip", "ds_norm.hip", "ds_choice.h", "ds_matmul.hip", "ds_join.hip",
+                  "ds_logprobs.hip", "ds_adamw.hip"),
 }
 
 
@@ -277,6 +325,17 @@ def _load() -> ctypes.CDLL:
         "ds_matmul": ([mat, mat, mat, P(ds_matmul_epilogue), vp, u64, vp], ctypes.c_int),
         "ds_activation_backward_workspace": ([i64, i64, P(u64)], ctypes.c_int),
         "ds_activation_backward": ([mat, mat, u32, mat, vp, vp, u64, vp], ctypes.c_int),
+        "ds_join_forward": ([P(ds_join), mat, mat, mat, mat, vp, vp, vp], ctypes.c_int),
+        "ds_join_backward_workspace": ([i64, i64, P(u64)], ctypes.c_int),
+        "ds_join_backward": ([P(ds_join), mat, mat, mat, mat, vp, vp, mat, mat, vp, vp, vp, vp, u64, vp], ctypes.c_int),
+        "ds_logprobs_workspace": ([mat, u32, P(u64)], ctypes.c_int),
+        "ds_logprobs": ([mat, ctypes.c_float, vp, vp, vp, vp, vp, u32, vp, vp, vp, u64, vp], ctypes.c_int),
+        "ds_logprobs_backward": ([mat, ctypes.c_float, vp, vp, vp, vp, vp, vp, mat, vp], ctypes.c_int),
+        "ds_adamw_create": ([P(ds_adamw_tensor), sz, P(vp)], ctypes.c_int),
+        "ds_adamw_destroy": ([vp], ctypes.c_int),
+        "ds_adamw_squares_workspace": ([vp, P(u64)], ctypes.c_int),
+        "ds_adamw_squares": ([vp, vp, vp, u64, vp], ctypes.c_int),
+        "ds_adamw_step": ([vp, P(ds_adamw_settings), vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -757,12 +816,22 @@ def make_matrix(tensor) -> ds_matrix:
 def make_mx8(codes, scale) -> ds_matrix:
     """A checkpoint in 8 bits out of two torch tensors on the GPU: int8 codes [rows, cols] and uint8 scales
     [rows, ceil(cols / 32)], both with neighbouring columns next to each other."""
+    return _make_eight(codes, scale, DS_MX8)
+
+
+def make_uf8(codes, scale) -> ds_matrix:
+    """Values from 0 on in 8 bits, out of uint8 codes and scales as make_mx8's."""
+    return _make_eight(codes, scale, DS_UF8)
+
+
+def _make_eight(codes, scale, dtype: int) -> ds_matrix:
     global _byte_types
     if not _byte_types:
         import torch
         _byte_types = (torch.int8, torch.uint8)
-    if codes.dtype is not _byte_types[0] or scale.dtype is not _byte_types[1]:
-        raise TypeError("codes are int8, scales uint8")
+    signed = dtype == DS_MX8
+    if codes.dtype is not _byte_types[0 if signed else 1] or scale.dtype is not _byte_types[1]:
+        raise TypeError(f"codes are {'int8' if signed else 'uint8'}, scales uint8")
     if not (codes.is_cuda and scale.is_cuda):
         raise ValueError("codes and scales are in device memory")
     if codes.dim() != 2 or scale.dim() != 2:
@@ -772,7 +841,7 @@ def make_mx8(codes, scale) -> ds_matrix:
         raise ValueError(f"codes of {rows} x {cols} have scales of {rows} x {-(-cols // 32)}, not {lines} x {groups}")
     if groups > 1 and across != 1:
         raise ValueError("the scales of a row are not next to each other")
-    return ds_matrix(codes.data_ptr(), DS_MX8, 0, rows, cols, *codes.stride(), scale.data_ptr(), down)
+    return ds_matrix(codes.data_ptr(), dtype, 0, rows, cols, *codes.stride(), scale.data_ptr(), down)
 
 
 def _vector(v, dtype: int, matrix: ds_matrix, axis: str, what: str):
@@ -872,3 +941,166 @@ def ds_activation_backward(dy: ds_matrix, z: ds_matrix, act: int, dz: ds_matrix,
     if type(dbias) is not int:
         dbias = _vector(dbias, DS_F32, dy, "cols", "dbias")
     _check(_lib.ds_activation_backward(dy, z, act, dz, dbias, workspace, workspace_bytes, stream), "ds_activation_backward")
+
+
+# ---- joints, log probabilities, the update
+
+def make_join(after: bool = False, after_gamma=None, gate=None, before: bool = False, before_gamma=None, keep: float = 1.0, scale: float = 1.0,
+              eps: float = 1e-6) -> ds_join:
+    """Which norms a joint has, and its vectors: 1-D torch tensors on the GPU, contiguous, of one type, with an element for each column.
+    (The structure keeps no tensor's memory.)"""
+    made = ds_join(None, None, None, DS_F32, (DS_JOIN_AFTER if after else 0) | (DS_JOIN_BEFORE if before else 0), keep, scale, eps)
+    lengths, kind = [], None
+    for what, v in (("after_gamma", after_gamma), ("gate", gate), ("before_gamma", before_gamma)):
+        if v is None:
+            continue
+        if not v.is_cuda:
+            raise ValueError(f"{what} is not in device memory")
+        if v.dim() != 1 or (v.shape[0] > 1 and v.stride(0) != 1):
+            raise ValueError(f"{what} is one contiguous dimension")
+        code = _float_code(v.dtype)
+        if kind is not None and code != kind:
+            raise TypeError("the vectors of a joint are of one type")
+        made.param_dtype = kind = code
+        setattr(made, what, v.data_ptr())
+        lengths.append((what, v.shape[0]))
+    made.vectors = tuple(lengths)
+    return made
+
+
+def _fits(join: ds_join, cols: int) -> None:
+    for what, length in join.vectors:
+        if length != cols:
+            raise ValueError(f"{what} has {length} elements for {cols} columns")
+
+
+def ds_join_forward(join: ds_join, u: Optional[ds_matrix], x: ds_matrix, out: Optional[ds_matrix], y: Optional[ds_matrix], rstd_after=None,
+                    rstd_before=None, stream: int = 0) -> None:
+    _fits(join, x.cols)
+    rstd_after, rstd_before = _vector(rstd_after, DS_F32, x, "rows", "rstd_after"), _vector(rstd_before, DS_F32, x, "rows", "rstd_before")
+    _check(_lib.ds_join_forward(join, u, x, out, y, rstd_after, rstd_before, stream), "ds_join_forward")
+
+
+def ds_join_backward_workspace(rows: int, cols: int) -> int:
+    out = ctypes.c_uint64(0)
+    _check(_lib.ds_join_backward_workspace(rows, cols, out), "ds_join_backward_workspace")
+    return out.value
+
+
+def ds_join_backward(join: ds_join, dout: Optional[ds_matrix], dy: Optional[ds_matrix], u: Optional[ds_matrix], out: Optional[ds_matrix], rstd_after,
+                     rstd_before, du: Optional[ds_matrix], dx: Optional[ds_matrix], dafter=None, dgate=None, dbefore=None,
+                     workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
+    like = dy if dy is not None else dout
+    if like is not None:
+        _fits(join, like.cols)
+        rstd_after, rstd_before = _vector(rstd_after, DS_F32, like, "rows", "rstd_after"), _vector(rstd_before, DS_F32, like, "rows", "rstd_before")
+        dafter, dgate = _vector(dafter, DS_F32, like, "cols", "dafter"), _vector(dgate, DS_F32, like, "cols", "dgate")
+        dbefore = _vector(dbefore, DS_F32, like, "cols", "dbefore")
+    _check(_lib.ds_join_backward(join, dout, dy, u, out, rstd_after, rstd_before, du, dx, dafter, dgate, dbefore, workspace, workspace_bytes, stream),
+           "ds_join_backward")
+
+
+_token_type = None
+
+
+def _tokens(v, shape, what: str):
+    """The address of whole numbers: an address as it is, or that of a contiguous int64 torch tensor on the GPU of this shape."""
+    global _token_type
+    if v is None or not hasattr(v, "data_ptr"):
+        return v
+    if _token_type is None:
+        import torch
+        _token_type = torch.int64
+    if v.dtype is not _token_type:
+        raise TypeError(f"{what} is {v.dtype}, not int64")
+    return _table(v, shape, what)
+
+
+def _table(v, shape, what: str):
+    if not v.is_cuda:
+        raise ValueError(f"{what} is not in device memory")
+    if tuple(v.shape) != shape or not v.is_contiguous():
+        raise ValueError(f"{what} is contiguous and {shape}, not {tuple(v.shape)} of strides {tuple(v.stride())}")
+    return v.data_ptr()
+
+
+def ds_logprobs_workspace(logits: ds_matrix, top: int = 0) -> int:
+    out = ctypes.c_uint64(0)
+    _check(_lib.ds_logprobs_workspace(logits, top, out), "ds_logprobs_workspace")
+    return out.value
+
+
+def ds_logprobs(logits: ds_matrix, scale: float, tokens, logprob, largest=None, logsum=None, entropy=None, top: int = 0, top_tokens=None,
+                top_logprobs=None, workspace: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
+    tokens = _tokens(tokens, (logits.rows,), "tokens")
+    logprob, largest = _vector(logprob, DS_F32, logits, "rows", "logprob"), _vector(largest, DS_F32, logits, "rows", "largest")
+    logsum, entropy = _vector(logsum, DS_F32, logits, "rows", "logsum"), _vector(entropy, DS_F32, logits, "rows", "entropy")
+    top_tokens = _tokens(top_tokens, (logits.rows, top), "top_tokens")
+    if hasattr(top_logprobs, "data_ptr"):
+        if _float_code(top_logprobs.dtype) != DS_F32:
+            raise TypeError(f"top_logprobs is {top_logprobs.dtype}, not float32")
+        top_logprobs = _table(top_logprobs, (logits.rows, top), "top_logprobs")
+    _check(_lib.ds_logprobs(logits, scale, tokens, logprob, largest, logsum, entropy, top, top_tokens, top_logprobs, workspace, workspace_bytes,
+                            stream), "ds_logprobs")
+
+
+def ds_logprobs_backward(logits: ds_matrix, scale: float, tokens, largest, logsum, entropy, dlogprob, dentropy, dlogits: ds_matrix,
+                         stream: int = 0) -> None:
+    tokens = _tokens(tokens, (logits.rows,), "tokens")
+    largest, logsum = _vector(largest, DS_F32, logits, "rows", "largest"), _vector(logsum, DS_F32, logits, "rows", "logsum")
+    entropy, dlogprob = _vector(entropy, DS_F32, logits, "rows", "entropy"), _vector(dlogprob, DS_F32, logits, "rows", "dlogprob")
+    dentropy = _vector(dentropy, DS_F32, logits, "rows", "dentropy")
+    _check(_lib.ds_logprobs_backward(logits, scale, tokens, largest, logsum, entropy, dlogprob, dentropy, dlogits, stream), "ds_logprobs_backward")
+
+
+def make_adamw_tensor(param: ds_matrix, grad: ds_matrix, m: ds_matrix, v: ds_matrix, copy: Optional[ds_matrix] = None, decay: float = 0.0,
+                      rate: float = 1.0) -> ds_adamw_tensor:
+    """One tensor of an update, of matrices by make_matrix (moments in 8 bits: by make_mx8 and make_uf8).  The caller keeps the memory alive for as
+    long as the table is used."""
+    return ds_adamw_tensor(param, grad, m, v, copy if copy is not None else ds_matrix(), decay, rate)
+
+
+def ds_adamw_create(tensors: Sequence[ds_adamw_tensor]) -> int:
+    out = ctypes.c_void_p(0)
+    table = (ds_adamw_tensor * max(len(tensors), 1))(*tensors)
+    _check(_lib.ds_adamw_create(table, len(tensors), ctypes.byref(out)), "ds_adamw_create")
+    return int(out.value)
+
+
+def ds_adamw_destroy(table: int) -> None:
+    _check(_lib.ds_adamw_destroy(table), "ds_adamw_destroy")
+
+
+def ds_adamw_squares_workspace(table: int) -> int:
+    out = ctypes.c_uint64(0)
+    _check(_lib.ds_adamw_squares_workspace(table, out), "ds_adamw_squares_workspace")
+    return out.value
+
+
+def _one(v, dtype: str, what: str):
+    """The address of a number in device memory: an address as it is, or that of a torch tensor of one element."""
+    if v is None or not hasattr(v, "data_ptr"):
+        return v
+    if str(v.dtype) != "torch." + dtype:
+        raise TypeError(f"{what} is {v.dtype}, not {dtype}")
+    if not v.is_cuda:
+        raise ValueError(f"{what} is not in device memory")
+    if v.numel() != 1:
+        raise ValueError(f"{what} is one number, not {v.numel()}")
+    return v.data_ptr()
+
+
+def make_adamw_settings(step, rate: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0, squares=None,
+                        most_norm: float = 0.0, seed: int = 0, rate_now=None) -> ds_adamw_settings:
+    """`step` (int64), `squares` (float64) and `rate_now` (float32): torch tensors of one element on the GPU, or addresses.  (The structure keeps
+    no tensor's memory.)"""
+    return ds_adamw_settings(rate, beta1, beta2, eps, grad_scale, most_norm, seed, _one(step, "int64", "step"), _one(rate_now, "float32", "rate_now"),
+                             _one(squares, "float64", "squares"))
+
+
+def ds_adamw_squares(table: int, squares, workspace: Optional[int], workspace_bytes: int, stream: int = 0) -> None:
+    _check(_lib.ds_adamw_squares(table, _one(squares, "float64", "squares"), workspace, workspace_bytes, stream), "ds_adamw_squares")
+
+
+def ds_adamw_step(table: int, settings: ds_adamw_settings, stream: int = 0) -> None:
+    _check(_lib.ds_adamw_step(table, settings, stream), "ds_adamw_step")

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdatastates_hip.so")
 SOURCES = ["ds_plan.cpp", "ds_kernels.hip", "ds_engine.cpp", "ds_file.cpp", "ds_ckpt.cpp",
-           "ds_mx8.hip", "ds_norm.hip", "ds_matmul.hip"]
+           "ds_mx8.hip", "ds_norm.hip", "ds_matmul.hip", "ds_join.hip", "ds_logprobs.hip", "ds_adamw.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-pthread",

@@ -21,30 +21,32 @@ constexpr int kThreads = 256;
 // Work items are pieces of eight columns; a row has a multiple of four of them, so that a group's are four neighbouring lanes.
 // (A division in 64 bits takes as long as the rest.  Index: uint32_t where it holds their number; `shift` is the binary logarithm of
 // `pieces`, or -1 where that is none.)
-template <typename T, typename Index>
+template <typename T, typename As, typename Index>
 __global__ __launch_bounds__(kThreads) void ds_mx8_save_kernel(Rows x, Rows saved, int64_t rows, int64_t cols, uint32_t pieces, int shift) {
   for (int64_t first = (int64_t)blockIdx.x * kThreads; first < rows * pieces; first += (int64_t)gridDim.x * kThreads) {
     const Index item = (Index)(first + threadIdx.x), row = shift >= 0 ? item >> shift : item / (Index)pieces;
     const int64_t i = row, j = (int64_t)(item - row * (Index)pieces) * 8, left = i < rows ? cols - j : 0;
     const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
-    mx8_put(saved, i, j, n, RowsOf<T>::get(x, i, j, n));
+    if (std::is_same<As, Mx8>::value) mx8_put(saved, i, j, n, RowsOf<T>::get(x, i, j, n));
+    else uf8_put(saved, i, j, n, RowsOf<T>::get(x, i, j, n));
   }
 }
 
-template <typename T, typename Index>
+template <typename T, typename As, typename Index>
 __global__ __launch_bounds__(kThreads) void ds_mx8_load_kernel(Rows saved, Rows x, int64_t rows, int64_t cols, uint32_t pieces, int shift) {
   for (int64_t first = (int64_t)blockIdx.x * kThreads; first < rows * pieces; first += (int64_t)gridDim.x * kThreads) {
     const Index item = (Index)(first + threadIdx.x), row = shift >= 0 ? item >> shift : item / (Index)pieces;
     const int64_t i = row, j = (int64_t)(item - row * (Index)pieces) * 8, left = i < rows ? cols - j : 0;
     const int n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
-    put_up_to8<T>(x.base, i * x.stride + j, n, RowsOf<Mx8>::get(saved, i, j, n));
+    put_up_to8<T>(x.base, i * x.stride + j, n, RowsOf<As>::get(saved, i, j, n));
   }
 }
 
 int check_pair(const ds_matrix *x, const ds_matrix *saved) {
   DS_TRY(ds_check_matrix(x, true));
-  DS_TRY(ds_check_matrix(saved, true));
-  return x->dtype == DS_MX8 || saved->dtype != DS_MX8 || !ds_same_extents(x, saved) ? DS_EINVAL : DS_OK;
+  const bool uf8 = saved && saved->dtype == DS_UF8;
+  DS_TRY(uf8 ? ds_check_uf8(saved) : ds_check_matrix(saved, true));
+  return x->dtype == DS_MX8 || (!uf8 && saved->dtype != DS_MX8) || !ds_same_extents(x, saved) ? DS_EINVAL : DS_OK;
 }
 
 template <bool SAVE>
@@ -62,8 +64,12 @@ int launch_mx8(const ds_matrix *x, const ds_matrix *saved, hipStream_t stream) {
       DS_HIP_TRY(hipGetLastError());
       return DS_OK;
     };
-    if (SAVE) return narrow ? launch(ds_mx8_save_kernel<T, uint32_t>, x, saved) : launch(ds_mx8_save_kernel<T, uint64_t>, x, saved);
-    return narrow ? launch(ds_mx8_load_kernel<T, uint32_t>, saved, x) : launch(ds_mx8_load_kernel<T, uint64_t>, saved, x);
+    const auto as = [&](auto format) -> int {
+      typedef decltype(format) As;
+      if (SAVE) return narrow ? launch(ds_mx8_save_kernel<T, As, uint32_t>, x, saved) : launch(ds_mx8_save_kernel<T, As, uint64_t>, x, saved);
+      return narrow ? launch(ds_mx8_load_kernel<T, As, uint32_t>, saved, x) : launch(ds_mx8_load_kernel<T, As, uint64_t>, saved, x);
+    };
+    return saved->dtype == DS_UF8 ? as(Uf8()) : as(Mx8());
   });
 }
 

@@ -44,6 +44,14 @@ inline int ds_check_matrix(const ds_matrix *m, bool rows_only) {
   return DS_OK;
 }
 
+// DS_UF8 is laid out as DS_MX8 is; no function takes it that does not ask for it by this.
+inline int ds_check_uf8(const ds_matrix *m) {
+  if (!m || m->dtype != DS_UF8) return DS_EINVAL;
+  ds_matrix like = *m;
+  like.dtype = DS_MX8;
+  return ds_check_matrix(&like, true);
+}
+
 inline bool ds_same_extents(const ds_matrix *a, const ds_matrix *b) { return a->rows == b->rows && a->cols == b->cols; }
 inline bool ds_misaligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
 
@@ -325,11 +333,58 @@ struct RowsOf<Mx8> {
   static __device__ inline Eight get(const Rows &m, int64_t i, int64_t j, int n) { return value(ask(m, i, j, n), n); }
 };
 
-// Leaves eight values (n <= 8 of them in the row, the others 0) of row i from column j on in a checkpoint.  All lanes of
-// the wavefront take part; four neighbouring ones hold a group.
-__device__ inline void mx8_put(const Rows &m, int64_t i, int64_t j, int n, const Eight &e) {
-  const uint32_t scale = mx8_scale(max_of_four_lanes(magnitude8(e)));
-  const ds_u32x2 q = mx8_codes(e, scale);
+// ---- device: values from 0 on in 8 bits ------------------------------------------------------------------------
+
+// Marks their type where a template takes an element type.
+struct Uf8 {};
+
+// The byte of a group whose largest value has these bits; `top` is 0x7f800000 or more where one is negative or no number (the sign is
+// the largest bit).
+__device__ inline uint32_t uf8_scale(uint32_t top) {
+  return top >= 0x7f800000u ? 255u : top >> 23 > 30u ? (top >> 23) - 30u : 0u;
+}
+// The code of a value of these bits, to which `round` of 2^20 parts of a step is added.
+__device__ inline uint32_t uf8_code(uint32_t bits, uint32_t round, uint32_t scale) {
+  const int most = min(255, 2039 - 8 * (int)scale), code = (int)((bits + round) >> 20) - 8 * (int)scale;
+  return bits == 0 || scale == 255u ? 0u : (uint32_t)(code < 1 ? 1 : code > most ? most : code);
+}
+__device__ inline float uf8_value(uint32_t code, uint32_t scale) {
+  return scale == 255u ? __uint_as_float(0x7fc00000u) : code == 0 ? 0.f : __uint_as_float((code + 8u * scale) << 20);
+}
+__device__ inline Eight uf8_values(ds_u32x2 codes, uint32_t scale) {
+  Eight e;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) e.v[k] = uf8_value(codes[k / 4] >> (8 * (k % 4)) & 255u, scale);
+  return e;
+}
+// The largest bits of eight values, -0 as 0.
+__device__ inline uint32_t largest_bits8(const Eight &e) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t b = __float_as_uint(e.v[k] + 0.f);
+    top = b > top ? b : top;
+  }
+  return top;
+}
+
+template <>
+struct RowsOf<Uf8> {
+  typedef RowsOf<Mx8>::Bits Bits;
+  static __device__ inline Bits ask(const Rows &m, int64_t i, int64_t j, int n) { return RowsOf<Mx8>::ask(m, i, j, n); }
+  static __device__ inline Eight value(const Bits &b, int n) {
+    Eight e = uf8_values(b.codes, b.scale);
+    if (n < 8) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) e.v[k] = k < n ? e.v[k] : 0.f;
+    }
+    return e;
+  }
+  static __device__ inline Eight get(const Rows &m, int64_t i, int64_t j, int n) { return value(ask(m, i, j, n), n); }
+};
+
+// Writes eight codes, and the byte of their group if they begin it.
+__device__ inline void eight_put(const Rows &m, int64_t i, int64_t j, int n, ds_u32x2 q, uint32_t scale) {
   if (n <= 0) return;
   uint8_t *codes = (uint8_t *)m.base + i * m.stride + j;
   if (n >= 8) *(ds_u32x2 *)codes = q;
@@ -338,6 +393,24 @@ __device__ inline void mx8_put(const Rows &m, int64_t i, int64_t j, int n, const
     for (int k = 0; k < 8; ++k)
       if (k < n) codes[k] = (uint8_t)(q[k / 4] >> (8 * (k % 4)));
   if (j % kGroup == 0) m.scale[i * m.scale_stride + j / kGroup] = (uint8_t)scale;
+}
+// Leaves eight values, rounded to the nearest code, as mx8_put does.
+__device__ inline void uf8_put(const Rows &m, int64_t i, int64_t j, int n, const Eight &e) {
+  const uint32_t scale = uf8_scale(max_of_four_lanes(largest_bits8(e)));
+  ds_u32x2 q = {0, 0};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t bits = __float_as_uint(e.v[k] + 0.f);
+    q[k / 4] |= uf8_code(bits, 0x7ffffu + (bits >> 20 & 1u), scale) << (8 * (k % 4));
+  }
+  eight_put(m, i, j, n, q, scale);
+}
+
+// Leaves eight values (n <= 8 of them in the row, the others 0) of row i from column j on in a checkpoint.  All lanes of
+// the wavefront take part; four neighbouring ones hold a group.
+__device__ inline void mx8_put(const Rows &m, int64_t i, int64_t j, int n, const Eight &e) {
+  const uint32_t scale = mx8_scale(max_of_four_lanes(magnitude8(e)));
+  eight_put(m, i, j, n, mx8_codes(e, scale), scale);
 }
 
 // ---- device: activations ---------------------------------------------------------------------------------------
