@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 #include <new>
 #include <type_traits>
 #include <utility>
@@ -20,24 +21,25 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kEach = 2;                     // pieces of a thread
-constexpr int64_t kPieces = kThreads * kEach;  // of a chunk
-constexpr int64_t kSquareGroups = 2048;      // work-groups of the sum of squares, for each kind of tensors
+constexpr int kEach = 2;                       // quads of a thread
+constexpr int64_t kQuads = kThreads * kEach;   // of a chunk
+constexpr int64_t kStream = 4 << 20;           // elements of a table from which on accesses are not temporal
+constexpr int64_t kSquareGroups = 2048;        // work-groups of the sum of squares, for each kind of tensors
 
-// A tensor in the table.  Its matrices are one row where that is how they lie.
+// A tensor in the table.  Its matrices are one row where that is how they lie; their strides are then not looked at.
 struct Tensor {
   Rows param, grad, m, v, copy;
-  int64_t rows, cols, pieces;  // pieces of a row: a multiple of four where moments have 8 bits
+  int64_t rows, cols, quads;  // quads of a row: a multiple of eight where moments have 8 bits
   uint32_t number, copy_dtype;
   float decay, rate;
 };
 struct Chunk {
-  int64_t piece;  // the first one
+  int64_t quad;  // the first one
   uint32_t tensor, reserved;
 };
-// A kind of tensors: their types, and their chunks.
+// A kind of tensors: their types, whether they are one row, and their chunks.
 struct Kind {
-  uint32_t param, grad, eight;
+  uint32_t param, grad, eight, flat;
   int64_t begin, end;
 };
 
@@ -58,22 +60,25 @@ __host__ __device__ inline uint32_t mix(uint32_t x) {
   return x ^ x >> 16;
 }
 
+// What all elements share.
 struct Now {
   float rate;      // settings'
   float step;      // 1 / (1 - beta1^t)
   float root;      // 1 / sqrt(1 - beta2^t)
-  float grad;      // what a gradient is multiplied with
   uint32_t key;    // mix(t + mix(seed))
+  float grad;      // what a gradient is multiplied with
   uint32_t still;  // nothing is to change
 };
 
-__device__ inline Now now_of(const Settings &s) {
-  Now w;
+// By one wavefront each, into `w`.  beta^t - 1 is off by as much of itself as t log(beta), its argument, is at most.
+__device__ inline void now_of_step(const Settings &s, Now &w) {
   const int64_t at = *s.step, t = at < 1 ? 1 : at;
   w.rate = s.rate_now ? *s.rate_now : (float)s.rate;
   w.key = mix((uint32_t)t + s.seed);
-  w.step = (float)(-1.0 / expm1((double)t * s.log_beta1));
-  w.root = (float)(1.0 / sqrt(-expm1((double)t * s.log_beta2)));
+  w.step = -1.f / expm1f((float)((double)t * s.log_beta1));
+  w.root = 1.f / sqrtf(-expm1f((float)((double)t * s.log_beta2)));
+}
+__device__ inline void now_of_gradients(const Settings &s, Now &w) {
   w.still = 0;
   double c = s.grad_scale;
   if (s.squares) {
@@ -82,98 +87,294 @@ __device__ inline Now now_of(const Settings &s) {
     if (s.most_norm > 0.0 && norm > s.most_norm) c = c * s.most_norm / norm;
   }
   w.grad = (float)c;
-  return w;
 }
 
-// Where piece `item` of a tensor is: its row, its first column, and how many columns of it are there.
+// An address that comes out of a table is one of global memory; the compiler knows that of arguments only, and would otherwise use flat
+// accesses, which wait for the scalar loads too.
+template <typename T>
+__device__ inline T *global(T *p) {
+  return (T *)(__attribute__((address_space(1))) T *)(uintptr_t)p;
+}
+__device__ inline Rows rows_of(const Rows &r) { return Rows{global(r.base), r.stride, global(r.scale), r.scale_stride}; }
+
+// Four neighbouring elements: a wavefront's access of 32-bit elements is then 1 KiB without a gap, which non-temporal accesses need.
+struct Four {
+  float v[4];
+};
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x1 __attribute__((aligned(1)));
+template <typename T>
+struct QuadOf;
+template <>
+struct QuadOf<float> {
+  typedef uint32_t Bits __attribute__((ext_vector_type(4)));
+  typedef u32x4 Memory;
+  typedef uint32_t One;
+  static __device__ inline Bits one(uint32_t x, int k) { Bits b = {0, 0, 0, 0}; b[k] = x; return b; }
+  static __device__ inline uint32_t part(const Bits &b, int k) { return b[k]; }
+  static __device__ inline Four value(const Bits &b) { return Four{{__uint_as_float(b[0]), __uint_as_float(b[1]), __uint_as_float(b[2]), __uint_as_float(b[3])}}; }
+  static __device__ inline Bits bits(const Four &x) { return Bits{__float_as_uint(x.v[0]), __float_as_uint(x.v[1]), __float_as_uint(x.v[2]), __float_as_uint(x.v[3])}; }
+};
+struct QuadOfHalves {
+  typedef uint32_t Bits __attribute__((ext_vector_type(2)));
+  typedef u32x2 Memory;
+  typedef uint16_t One;
+  static __device__ inline Bits one(uint32_t x, int k) { Bits b = {0, 0}; b[k / 2] = x << (16 * (k % 2)); return b; }
+  static __device__ inline uint32_t part(const Bits &b, int k) { return b[k / 2] >> (16 * (k % 2)) & 0xffffu; }
+};
+template <>
+struct QuadOf<__hip_bfloat16> : QuadOfHalves {
+  static __device__ inline Four value(const Bits &b) {
+    return Four{{__uint_as_float(b[0] << 16), __uint_as_float(b[0] & 0xffff0000u), __uint_as_float(b[1] << 16), __uint_as_float(b[1] & 0xffff0000u)}};
+  }
+  static __device__ inline Bits bits(const Four &x) {
+    return Bits{float_to_bf16(x.v[0]) | float_to_bf16(x.v[1]) << 16, float_to_bf16(x.v[2]) | float_to_bf16(x.v[3]) << 16};
+  }
+};
+template <>
+struct QuadOf<__half> : QuadOfHalves {
+  static __device__ inline Four value(const Bits &b) {
+    return Four{{f16_to_float(b[0] & 0xffffu), f16_to_float(b[0] >> 16), f16_to_float(b[1] & 0xffffu), f16_to_float(b[1] >> 16)}};
+  }
+  static __device__ inline Bits bits(const Four &x) {
+    return Bits{float_to_f16(x.v[0]) | float_to_f16(x.v[1]) << 16, float_to_f16(x.v[2]) | float_to_f16(x.v[3]) << 16};
+  }
+};
+template <>
+struct QuadOf<uint8_t> {  // codes
+  typedef uint32_t Bits;
+  typedef u32x1 Memory;
+  typedef uint8_t One;
+  static __device__ inline Bits one(uint32_t x, int k) { return x << (8 * k); }
+  static __device__ inline uint32_t part(const Bits &b, int k) { return b >> (8 * k) & 255u; }
+};
+// The first n <= 4 of the four from element `at` on; the others are 0, or not written.  STREAM: not temporal.
+template <typename T, bool STREAM>
+__device__ inline typename QuadOf<T>::Bits ask_quad(const void *base, int64_t at, int n) {
+  typedef QuadOf<T> Q;
+  typename Q::Bits b = {};
+  const typename Q::One *from = (const typename Q::One *)base + at;
+  if (n >= 4) return STREAM ? __builtin_nontemporal_load((const typename Q::Memory *)from) : *(const typename Q::Memory *)from;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (k < n) b |= Q::one(from[k], k);
+  return b;
+}
+template <typename T, bool STREAM>
+__device__ inline void put_quad(void *base, int64_t at, int n, const typename QuadOf<T>::Bits &b) {
+  typedef QuadOf<T> Q;
+  typename Q::One *to = (typename Q::One *)base + at;
+  if (n >= 4) {
+    if (STREAM) __builtin_nontemporal_store((typename Q::Memory)b, (typename Q::Memory *)to);
+    else *(typename Q::Memory *)to = b;
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (k < n) to[k] = (typename Q::One)Q::part(b, k);
+}
+
+// Where quad `item` of a tensor of rows is: its row, its first column, and how many columns of it are there.
 __device__ inline void place_of(const Tensor &t, int64_t item, int64_t &i, int64_t &j, int &n) {
-  if (t.rows == 1) i = 0, j = item;
-  else if (t.rows * t.pieces <= 0xffffffffll - kPieces) i = (uint32_t)item / (uint32_t)t.pieces, j = (uint32_t)item - (uint32_t)i * (uint32_t)t.pieces;
-  else i = item / t.pieces, j = item - i * t.pieces;
-  j *= 8;
+  if (t.rows * t.quads <= 0xffffffffll - kQuads) i = (uint32_t)item / (uint32_t)t.quads, j = (uint32_t)item - (uint32_t)i * (uint32_t)t.quads;
+  else i = item / t.quads, j = item - i * t.quads;
+  j *= 4;
   const int64_t left = i < t.rows ? t.cols - j : 0;
-  n = (int)(left < 0 ? 0 : left < 8 ? left : 8);
+  n = (int)(left < 0 ? 0 : left < 4 ? left : 4);
+}
+template <bool FLAT>
+__device__ inline void place(const Tensor &t, int64_t item, int64_t &i, int64_t &j, int &n) {
+  if (!FLAT) return place_of(t, item, i, j, n);
+  i = 0, j = item * 4;
+  const int64_t left = t.cols - j;
+  n = (int)(left < 0 ? 0 : left < 4 ? left : 4);
 }
 
-__device__ inline void put_copy(const Tensor &t, int64_t i, int64_t j, int n, const Eight &p) {
-  const int64_t at = i * t.copy.stride + j;
-  if (t.copy_dtype == DS_BF16) put_up_to8<__hip_bfloat16>(t.copy.base, at, n, p);
-  else if (t.copy_dtype == DS_F16) put_up_to8<__half>(t.copy.base, at, n, p);
-  else put_up_to8<float>(t.copy.base, at, n, p);
+// The largest of eight neighbouring lanes', which hold a group of 32.
+__device__ inline uint32_t max_of_eight_lanes(uint32_t m) {
+  m = max_of_four_lanes(m);
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xf, 0xf, true);  // the other half of eight, mirrored
+  return o > m ? o : m;
 }
 
-template <typename P, typename G, bool EIGHT>
-__global__ __launch_bounds__(kThreads) void ds_adamw_step_kernel(const Tensor *tensors, const Chunk *chunks, int64_t count, Settings s) {
-  typedef std::conditional_t<EIGHT, Mx8, float> M;
-  typedef std::conditional_t<EIGHT, Uf8, float> V;
+// sqrt(x) to a unit of the last place.  (The instruction takes no subnormal numbers.)
+__device__ inline float root_of(float x) {
+  const bool small = x < 0x1p-96f;
+  const float r = __builtin_amdgcn_sqrtf(small ? x * 0x1p64f : x);
+  return small ? r * 0x1p-32f : r;
+}
+
+// param, m and v (before they are rounded) after the step.
+__device__ inline void step_of(const Settings &s, const Now &w, float step, float decay, const Four &grad, Four &param, Four &first, Four &second) {
+  {
+    // rounded after each operation, so that a code, which the last bit may decide, is what the formula in 32 bits says anywhere
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float x = grad.v[k] * w.grad;
+      first.v[k] = first.v[k] * s.beta1 + x * s.rest1;
+      second.v[k] = second.v[k] * s.beta2 + x * x * s.rest2;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    param.v[k] -= decay * param.v[k] + step * first.v[k] * __builtin_amdgcn_rcpf(root_of(second.v[k]) * w.root + s.eps);
+}
+
+// Moments in 8 bits, and back, rounded at random: `at` is the number of the first of the four.  All lanes take part; `n`: how many there are.
+__device__ inline Four first_of(uint32_t codes, uint32_t scale) {
+  const float step = mx8_step(scale);
+  Four x;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x.v[k] = (float)((int)(codes << (24 - 8 * k)) >> 24) * step;
+  return x;
+}
+__device__ inline Four second_of(uint32_t codes, uint32_t scale) {
+  const float none = scale == 255u ? __uint_as_float(0x7fc00000u) : 0.f;
+  codes = scale == 255u ? 0u : codes;
+  Four x;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t c = codes >> (8 * k) & 255u;
+    x.v[k] = c ? __uint_as_float((c << 20) + (scale << 23)) : none;
+  }
+  return x;
+}
+__device__ inline void codes_of(const Four &first, const Four &second, uint32_t at, uint32_t &code_m, uint32_t &scale_m, uint32_t &code_v, uint32_t &scale_v) {
+  uint32_t top_m = 0, top_v = 0, bits[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    bits[k] = __float_as_uint(second.v[k]);
+    top_m = max(top_m, __float_as_uint(first.v[k]) & 0x7fffffffu), top_v = max(top_v, bits[k]);
+  }
+  scale_m = mx8_scale(max_of_eight_lanes(top_m)), scale_v = uf8_scale(max_of_eight_lanes(top_v));
+  const bool tiny = scale_m < 6u;  // 1 / step is no float: the values are made larger first
+  const float steps = __uint_as_float((tiny ? 229u - scale_m : 260u - (scale_m == 255u ? 133u : scale_m)) << 23), before = tiny ? 0x1p31f : 1.f;
+  const uint32_t base = scale_v << 23;
+  const int most = min(255, 2039 - 8 * (int)scale_v);
+  uint32_t q[4], c[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t r = mix(at + k);
+    const float u = __builtin_fmaf((float)(r & 0xffffu), 0x1p-16f, 0x1p-17f);
+    q[k] = (uint32_t)(int)__builtin_amdgcn_fmed3f(__builtin_floorf(__builtin_fmaf(first.v[k] * before, steps, u)), -127.f, 127.f);
+    // (what is 0 stays 0: the sum is then below a step, and below 0 where there is a base)
+    c[k] = (uint32_t)min(max((int)(bits[k] + (r >> 12 & 0xffff0u) + 8u - base) >> 20, (int)min(bits[k], 1u)), most);
+  }
+  const uint32_t low = __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400u), high = __builtin_amdgcn_perm(q[3], q[2], 0x04000c0cu);
+  code_m = (low | high) & (scale_m == 255u ? 0u : ~0u);
+  code_v = (c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24) & (scale_v == 255u ? 0u : ~0u);
+}
+
+// Where four elements are, from the bases on.
+struct Place {
+  int64_t param, grad, m, v, copy, m_scale, v_scale;
+  uint32_t at;  // their number in the tensor
+  int n;        // how many of them there are
+  bool first;   // of their group
+};
+template <int FULL>
+__device__ inline Place place_flat(uint32_t quad, int left, uint32_t at) {
+  const uint32_t j = quad * 4;
+  const int more = left - (int)j;
+  return Place{j, j, j, j, j, j / kGroup, j / kGroup, at + j, FULL ? 4 : more < 0 ? 0 : more < 4 ? more : 4, j % kGroup == 0};
+}
+__device__ inline Place place_rows(const Tensor &t, int64_t item) {
+  int64_t i, j;
+  int n;
+  place_of(t, item, i, j, n);
+  return Place{i * t.param.stride + j, i * t.grad.stride + j, i * t.m.stride + j, i * t.v.stride + j, i * t.copy.stride + j, i * t.m.scale_stride + j / kGroup,
+               i * t.v.scale_stride + j / kGroup, (uint32_t)(i * t.cols + j), n, j % kGroup == 0};
+}
+
+// A chunk.  FULL: all its quads are whole.
+template <typename P, typename G, bool EIGHT, bool FLAT, bool STREAM, bool FULL>
+__device__ inline void step_chunk(const Tensor &t, int64_t quad, int left, const Settings &s, Now &shared, bool begins) {
+  typedef std::conditional_t<EIGHT, uint8_t, float> M;
+  Place at[kEach];
+  typename QuadOf<P>::Bits p[kEach];
+  typename QuadOf<G>::Bits g[kEach];
+  typename QuadOf<M>::Bits m[kEach], v[kEach];
+  uint32_t m_scale[kEach], v_scale[kEach];
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    if (FLAT) at[e] = place_flat<FULL>(e * kThreads + threadIdx.x, left, (uint32_t)quad * 4);
+    else at[e] = place_rows(t, quad + e * kThreads + threadIdx.x);
+    const Place &o = at[e];
+    p[e] = ask_quad<P, STREAM>(t.param.base, o.param, o.n), g[e] = ask_quad<G, STREAM>(t.grad.base, o.grad, o.n);
+    m[e] = ask_quad<M, STREAM>(t.m.base, o.m, o.n), v[e] = ask_quad<M, STREAM>(t.v.base, o.v, o.n);
+    if (EIGHT) m_scale[e] = o.n > 0 ? t.m.scale[o.m_scale] : 0u, v_scale[e] = o.n > 0 ? t.v.scale[o.v_scale] : 0u;
+  }
+  if (begins) {
+    if (threadIdx.x / 64 == 0) now_of_step(s, shared);
+    if (threadIdx.x / 64 == 1) now_of_gradients(s, shared);
+    __syncthreads();
+  }
+  const Now w = shared;
+  if (w.still) return;
+  const float rate = w.rate * t.rate, step = rate * w.step, decay = rate * t.decay;
+  const uint32_t key = mix(t.number + w.key);
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const Place &o = at[e];
+    Four x = QuadOf<P>::value(p[e]), first, second;
+    if constexpr (EIGHT) first = first_of(m[e], m_scale[e]), second = second_of(v[e], v_scale[e]);
+    else first = QuadOf<float>::value(m[e]), second = QuadOf<float>::value(v[e]);
+    if (EIGHT && !FULL) {  // a step of NaN is not to reach the places beyond the row
+#pragma unroll
+      for (int k = 0; k < 4; ++k) first.v[k] = k < o.n ? first.v[k] : 0.f, second.v[k] = k < o.n ? second.v[k] : 0.f;
+    }
+    step_of(s, w, step, decay, QuadOf<G>::value(g[e]), x, first, second);
+    put_quad<P, STREAM>(t.param.base, o.param, o.n, QuadOf<P>::bits(x));
+    if (t.copy.base) {
+      if (t.copy_dtype == DS_BF16) put_quad<__hip_bfloat16, STREAM>(t.copy.base, o.copy, o.n, QuadOf<__hip_bfloat16>::bits(x));
+      else if (t.copy_dtype == DS_F16) put_quad<__half, STREAM>(t.copy.base, o.copy, o.n, QuadOf<__half>::bits(x));
+      else put_quad<float, STREAM>(t.copy.base, o.copy, o.n, QuadOf<float>::bits(x));
+    }
+    if constexpr (EIGHT) {
+      uint32_t code_m, code_v, scale_m, scale_v;
+      codes_of(first, second, o.at + key, code_m, scale_m, code_v, scale_v);
+      put_quad<uint8_t, STREAM>(t.m.base, o.m, o.n, code_m);
+      put_quad<uint8_t, STREAM>(t.v.base, o.v, o.n, code_v);
+      if (o.n > 0 && o.first) t.m.scale[o.m_scale] = (uint8_t)scale_m, t.v.scale[o.v_scale] = (uint8_t)scale_v;
+    } else {
+      put_quad<float, STREAM>(t.m.base, o.m, o.n, QuadOf<float>::bits(first));
+      put_quad<float, STREAM>(t.v.base, o.v, o.n, QuadOf<float>::bits(second));
+    }
+  }
+}
+
+template <typename T>
+__device__ inline void advance(Rows &r, int64_t j) {
+  r.base = (T *)r.base + j;
+  if (r.scale) r.scale += j / kGroup;
+}
+
+// A work-group takes a chunk, or several where a launch has no place for as many work-groups.
+template <typename P, typename G, bool EIGHT, bool FLAT, bool STREAM>
+__global__ __launch_bounds__(kThreads) void ds_adamw_step_kernel(const Tensor *__restrict__ tensors, const Chunk *__restrict__ chunks, int64_t count, Settings s) {
+  typedef std::conditional_t<EIGHT, uint8_t, float> M;
   __shared__ Now shared;
   for (int64_t c = blockIdx.x; c < count; c += gridDim.x) {
     const Chunk chunk = chunks[c];
-    const Tensor t = tensors[chunk.tensor];
-    int64_t i[kEach], j[kEach];
-    int n[kEach];
-    typename RowsOf<P>::Bits p[kEach];
-    typename RowsOf<G>::Bits g[kEach];
-    typename RowsOf<M>::Bits m[kEach];
-    typename RowsOf<V>::Bits v[kEach];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      place_of(t, chunk.piece + e * kThreads + threadIdx.x, i[e], j[e], n[e]);
-      p[e] = RowsOf<P>::ask(t.param, i[e], j[e], n[e]), g[e] = RowsOf<G>::ask(t.grad, i[e], j[e], n[e]);
-      m[e] = RowsOf<M>::ask(t.m, i[e], j[e], n[e]), v[e] = RowsOf<V>::ask(t.v, i[e], j[e], n[e]);
+    // whole, into scalar registers, before anything is written that it might be
+    Tensor t = tensors[chunk.tensor];
+    t.param = rows_of(t.param), t.grad = rows_of(t.grad), t.m = rows_of(t.m), t.v = rows_of(t.v), t.copy = rows_of(t.copy);
+    const bool begins = c == blockIdx.x;
+    if (!FLAT) {
+      step_chunk<P, G, EIGHT, FLAT, STREAM, false>(t, chunk.quad, 0, s, shared, begins);
+      continue;
     }
-    if (c == blockIdx.x) {
-      if (threadIdx.x < 64) {
-        const Now w = now_of(s);
-        if (threadIdx.x == 0) shared = w;
-      }
-      __syncthreads();
+    const int64_t j = chunk.quad * 4, more = t.cols - j;
+    advance<P>(t.param, j), advance<G>(t.grad, j), advance<M>(t.m, j), advance<M>(t.v, j);
+    if (t.copy.base) {
+      if (t.copy_dtype == DS_F32) advance<float>(t.copy, j);
+      else advance<uint16_t>(t.copy, j);
     }
-    const Now w = shared;
-    if (w.still) return;
-    const float rate = w.rate * t.rate, step = rate * w.step, decay = rate * t.decay;
-    const uint32_t key = mix(t.number + w.key);
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      Eight param = RowsOf<P>::value(p[e], n[e]), first = RowsOf<M>::value(m[e], n[e]), second = RowsOf<V>::value(v[e], n[e]);
-      const Eight grad = RowsOf<G>::value(g[e], n[e]);
-      {
-        // rounded after each operation, so that a code, which the last bit may decide, is what the formula in 32 bits says anywhere
-#pragma clang fp contract(off)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float x = grad.v[k] * w.grad;
-          first.v[k] = first.v[k] * s.beta1 + x * s.rest1;
-          second.v[k] = second.v[k] * s.beta2 + x * x * s.rest2;
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        param.v[k] -= decay * param.v[k] + step * first.v[k] / (sqrtf(second.v[k]) * w.root + s.eps);
-      }
-      put_up_to8<P>(t.param.base, i[e] * t.param.stride + j[e], n[e], param);
-      if (t.copy.base) put_copy(t, i[e], j[e], n[e], param);
-      if constexpr (EIGHT) {
-        const uint32_t at = (uint32_t)(i[e] * t.cols + j[e]) + key;
-        const uint32_t scale_m = mx8_scale(max_of_four_lanes(magnitude8(first)));
-        const uint32_t scale_v = uf8_scale(max_of_four_lanes(largest_bits8(second)));
-        ds_u32x2 code_m = {0, 0}, code_v = {0, 0};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t r = mix(at + k);
-          const float u = ((float)(r & 0xffffu) + 0.5f) * 0x1p-16f;
-          const float q = __builtin_floorf(ldexpf(first.v[k], 133 - (int)scale_m) + u);
-          const uint32_t byte = (uint32_t)(int)__builtin_amdgcn_fmed3f(q, -127.f, 127.f) & 255u;
-          code_m[k / 4] |= (scale_m == 0u || scale_m == 255u ? 0u : byte) << (8 * (k % 4));
-          code_v[k / 4] |= uf8_code(__float_as_uint(second.v[k]), (r >> 16 << 4) + 8u, scale_v) << (8 * (k % 4));
-        }
-        eight_put(t.m, i[e], j[e], n[e], code_m, scale_m);
-        eight_put(t.v, i[e], j[e], n[e], code_v, scale_v);
-      } else {
-        put_up_to8<float>(t.m.base, i[e] * t.m.stride + j[e], n[e], first);
-        put_up_to8<float>(t.v.base, i[e] * t.v.stride + j[e], n[e], second);
-      }
-    }
+    const int left = (int)(more < kQuads * 4 ? more : kQuads * 4);
+    if (left == kQuads * 4) step_chunk<P, G, EIGHT, FLAT, STREAM, true>(t, chunk.quad, left, s, shared, begins);
+    else step_chunk<P, G, EIGHT, FLAT, STREAM, false>(t, chunk.quad, left, s, shared, begins);
   }
 }
 
@@ -183,23 +384,31 @@ __device__ inline double wave_sum(double x) {
   return x;
 }
 
-// One sum for each work-group, in the order of its chunks.  (In 64 bits: gradients' squares span more than 32 bits' exponents do, and
-// the sums of ranks are added.)
-template <typename G>
-__global__ __launch_bounds__(kThreads) void ds_adamw_squares_kernel(const Tensor *tensors, const Chunk *chunks, int64_t count, double *partial) {
+// One sum for each work-group, in the order of its chunks; the next chunk's place is on its way while it adds.  (In 64 bits: gradients'
+// squares span more than 32 bits' exponents do, and the sums of ranks are added.)
+template <typename G, bool FLAT, bool STREAM>
+__global__ __launch_bounds__(kThreads) void ds_adamw_squares_kernel(const Tensor *__restrict__ tensors, const Chunk *__restrict__ chunks, int64_t count, double *partial) {
   __shared__ double sums[kThreads / 64];
   double sum = 0.0;
+  Chunk chunk = chunks[blockIdx.x];
+  Tensor t = tensors[chunk.tensor];
   for (int64_t c = blockIdx.x; c < count; c += gridDim.x) {
-    const Chunk chunk = chunks[c];
-    const Tensor &t = tensors[chunk.tensor];
+    const Rows grad = rows_of(t.grad);
+    typename QuadOf<G>::Bits g[kEach];
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       int64_t i, j;
       int n;
-      place_of(t, chunk.piece + e * kThreads + threadIdx.x, i, j, n);
-      const Eight g = RowsOf<G>::get(t.grad, i, j, n);
+      place<FLAT>(t, chunk.quad + e * kThreads + threadIdx.x, i, j, n);
+      g[e] = ask_quad<G, STREAM>(grad.base, i * (FLAT ? 0 : grad.stride) + j, n);
+    }
+    chunk = chunks[c + gridDim.x < count ? c + gridDim.x : c];
+    t = tensors[chunk.tensor];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sum += (double)g.v[k] * (double)g.v[k];
+    for (int e = 0; e < kEach; ++e) {
+      const Four x = QuadOf<G>::value(g[e]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum += (double)x.v[k] * (double)x.v[k];
     }
   }
   sum = wave_sum(sum);
@@ -256,6 +465,7 @@ struct ds_adamw {
   const Tensor *tensors = nullptr;
   const Chunk *chunks = nullptr;
   std::vector<Kind> kinds;
+  int64_t elements = 0;
   int64_t parts() const {
     int64_t sum = 0;
     for (const Kind &k : kinds) sum += square_groups(k);
@@ -302,6 +512,7 @@ int make_table(const ds_adamw_tensor *from, size_t n, ds_adamw &table) {
     DS_TRY(check_tensor(f, copied));
     const int64_t rows = f.param.rows, cols = f.param.cols;
     if (rows == 0 || cols == 0) continue;
+    table.elements += rows * cols;
     const bool eight = f.m.dtype == DS_MX8;
     const ds_matrix *all[] = {&f.param, &f.grad, &f.m, &f.v, copied ? &f.copy : nullptr};
     bool row = true;
@@ -314,9 +525,9 @@ int make_table(const ds_adamw_tensor *from, size_t n, ds_adamw &table) {
     Tensor t{};
     t.param = ds_rows(&f.param), t.grad = ds_rows(&f.grad), t.m = ds_rows(&f.m), t.v = ds_rows(&f.v), t.copy = ds_rows(copied ? &f.copy : nullptr);
     t.rows = row ? 1 : rows, t.cols = row ? rows * cols : cols;
-    t.pieces = eight ? ds_groups(t.cols) * (kGroup / 8) : (t.cols + 7) / 8;
+    t.quads = eight ? ds_groups(t.cols) * (kGroup / 4) : (t.cols + 3) / 4;
     t.number = (uint32_t)k, t.copy_dtype = copied ? f.copy.dtype : 0, t.decay = f.decay, t.rate = f.rate;
-    order.emplace_back(f.param.dtype * 6 + f.grad.dtype * 2 + eight, (uint32_t)tensors.size());
+    order.emplace_back(f.param.dtype * 12 + f.grad.dtype * 4 + eight * 2 + row, (uint32_t)tensors.size());
     tensors.push_back(t);
   }
   if (written_twice(written)) return DS_EOVERLAP;
@@ -324,15 +535,18 @@ int make_table(const ds_adamw_tensor *from, size_t n, ds_adamw &table) {
   std::vector<Chunk> chunks;
   for (size_t k = 0; k < order.size(); ++k) {
     const uint32_t kind = order[k].first, at = order[k].second;
-    if (k == 0 || order[k - 1].first != kind) table.kinds.push_back({kind / 6, kind / 2 % 3, kind % 2, (int64_t)chunks.size(), 0});
-    const int64_t all = tensors[at].rows * tensors[at].pieces;
-    for (int64_t piece = 0; piece < all; piece += kPieces) chunks.push_back({piece, at, 0});
+    if (k == 0 || order[k - 1].first != kind) table.kinds.push_back({kind / 12, kind / 4 % 3, kind / 2 % 2, kind % 2, (int64_t)chunks.size(), 0});
+    const int64_t all = tensors[at].rows * tensors[at].quads;
+    for (int64_t quad = 0; quad < all; quad += kQuads) chunks.push_back({quad, at, 0});
     table.kinds.back().end = (int64_t)chunks.size();
   }
   DS_HIP_TRY(hipGetDevice(&table.device));
   if (tensors.empty()) return DS_OK;
   const size_t first = tensors.size() * sizeof(Tensor), second = chunks.size() * sizeof(Chunk);
-  const hipError_t e = hipMalloc(&table.memory, first + second);
+  std::vector<uint8_t> all(first + second);
+  std::memcpy(all.data(), tensors.data(), first);
+  std::memcpy(all.data() + first, chunks.data(), second);
+  const hipError_t e = hipMalloc(&table.memory, all.size());
   if (e == hipErrorOutOfMemory) {
     (void)hipGetLastError();
     return DS_ENOMEM;
@@ -340,8 +554,7 @@ int make_table(const ds_adamw_tensor *from, size_t n, ds_adamw &table) {
   DS_HIP_TRY(e);
   table.tensors = (const Tensor *)table.memory;
   table.chunks = (const Chunk *)((const uint8_t *)table.memory + first);
-  DS_HIP_TRY(hipMemcpy(table.memory, tensors.data(), first, hipMemcpyHostToDevice));
-  DS_HIP_TRY(hipMemcpy((uint8_t *)table.memory + first, chunks.data(), second, hipMemcpyHostToDevice));
+  DS_HIP_TRY(hipMemcpy(table.memory, all.data(), all.size(), hipMemcpyHostToDevice));
   return DS_OK;
 }
 
@@ -401,10 +614,14 @@ extern "C" int ds_adamw_squares(const ds_adamw *table, double *squares, void *wo
     const int64_t groups = square_groups(k);
     DS_TRY(ds_with_type(k.grad, [&](auto type) -> int {
       typedef decltype(type) G;
-      hipLaunchKernelGGL(ds_adamw_squares_kernel<G>, dim3((uint32_t)groups), dim3(kThreads), 0, (hipStream_t)stream, table->tensors,
-                         table->chunks + k.begin, k.end - k.begin, partial);
-      DS_HIP_TRY(hipGetLastError());
-      return DS_OK;
+      const auto launch = [&](auto kernel) -> int {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(kThreads), 0, (hipStream_t)stream, table->tensors, table->chunks + k.begin,
+                           k.end - k.begin, partial);
+        DS_HIP_TRY(hipGetLastError());
+        return DS_OK;
+      };
+      if (!k.flat) return launch(ds_adamw_squares_kernel<G, false, false>);
+      return table->elements < kStream ? launch(ds_adamw_squares_kernel<G, true, false>) : launch(ds_adamw_squares_kernel<G, true, true>);
     }));
     partial += groups;
   }
@@ -425,17 +642,22 @@ extern "C" int ds_adamw_step(const ds_adamw *table, const ds_adamw_settings *set
   const Settings s{f.rate, std::log(f.beta1), std::log(f.beta2), f.grad_scale, f.most_norm, f.step, f.rate_now, f.squares, (float)f.beta1,
                    (float)f.beta2, (float)(1.0 - f.beta1), (float)(1.0 - f.beta2), (float)f.eps, mix((uint32_t)f.seed ^ mix((uint32_t)(f.seed >> 32)))};
   for (const Kind &k : table->kinds) {
-    const int64_t count = k.end - k.begin, grid = std::min(count, kMaxGrid);
+    const int64_t count = k.end - k.begin;
     DS_TRY(ds_with_type(k.param, [&](auto type) -> int {
       typedef decltype(type) P;
       return ds_with_type(k.grad, [&](auto grad) -> int {
         typedef decltype(grad) G;
         const auto launch = [&](auto kernel) -> int {
-          hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(kThreads), 0, (hipStream_t)stream, table->tensors, table->chunks + k.begin, count, s);
+          hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(count, kMaxGrid)), dim3(kThreads), 0, (hipStream_t)stream, table->tensors,
+                             table->chunks + k.begin, count, s);
           DS_HIP_TRY(hipGetLastError());
           return DS_OK;
         };
-        return k.eight ? launch(ds_adamw_step_kernel<P, G, true>) : launch(ds_adamw_step_kernel<P, G, false>);
+        if (!k.flat)
+          return k.eight ? launch(ds_adamw_step_kernel<P, G, true, false, false>) : launch(ds_adamw_step_kernel<P, G, false, false, false>);
+        if (table->elements < kStream)
+          return k.eight ? launch(ds_adamw_step_kernel<P, G, true, true, false>) : launch(ds_adamw_step_kernel<P, G, false, true, false>);
+        return k.eight ? launch(ds_adamw_step_kernel<P, G, true, true, true>) : launch(ds_adamw_step_kernel<P, G, false, true, true>);
       });
     }));
   }
