@@ -1,16 +1,16 @@
 // Log probabilities of tokens: forward, with entropy and the likeliest tokens, and backward.
 //
 // Both are bound by HBM: forward reads the logits once, backward reads them and writes their gradient.  A row belongs to one
-// to sixteen wavefronts, whose threads have pieces of eight neighbouring columns; each thread keeps, of what it has seen, the
+// to sixteen wavefronts, whose threads have pieces of neighbouring columns, 16 bytes each; each thread keeps, of what it has seen, the
 // largest logit m, s = sum exp(scale (x - m)) and t = sum exp(scale (x - m)) (x - m), and where m grows it multiplies them
 // by exp of the difference (t after the difference times s was added).  Threads' triples are joined by the same rule, in an order
 // that only the row's length decides.  Then logsum = log(s) and entropy = logsum - scale t / s.
 //
-// The likeliest: the lanes of a row are 64 sets; the `top`-th largest of the sets' largest logits is one that at least `top` columns
-// reach, so the columns that reach it contain those wanted, and mostly few others.  The threads that have such columns read theirs
-// again, out of the caches, and put them into LDS, where each is ranked by counting those in front of it.  Columns are in the
-// order of a key of their logit and place, which no two share.  Where more columns reach the bound than LDS has room for
-// (many equal ones, or few columns that are not masked), the row is read once for each rank instead.
+// The likeliest: the largest logit of every piece goes to LDS.  The lanes of a row are 8, 16 or 32 sets, `top` at least; as many columns
+// reach the least of the sets' largest logits, so the pieces that reach it contain those wanted, and mostly few others.  These pieces are
+// read again, one by each thread, and what reaches the bound is put into LDS, where each is ranked by counting those in front of it.
+// Columns are in the order of a key of their logit and place, which no two share.  Where more reach the bound than LDS has room for (many
+// equal ones, rows in order, few columns that are not masked), the `top`-th of the first 256 found is a higher bound, and it is tried again.
 //
 // Few rows are cut into parts, one work-group each, whose triples and likeliest a second launch joins.
 
@@ -25,7 +25,8 @@ namespace {
 constexpr float kInf = __builtin_inff();
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kCandidates = 1024;
+constexpr int kCandidates = 512, kSample = 256;  // room for columns that may be among the likeliest, and for pieces that have such
+constexpr int kMostPieces = 8192;                // of a row, or a part, whose likeliest are looked for
 
 struct Triple {
   float m, s, t;
@@ -42,25 +43,66 @@ __device__ inline void raise(Triple &a, float m, float c) {
   a.s *= f;
   a.m = m;
 }
-template <bool ENTROPY>
-__device__ inline Triple join(Triple a, Triple b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  raise<ENTROPY>(a, m, c), raise<ENTROPY>(b, m, c);
-  return {m, a.s + b.s, a.t + b.t};
-}
-template <bool ENTROPY>
-__device__ inline void add8(Triple &a, const Eight &x, float c) {
-  float m = a.m;
+// A piece: 16 bytes, 8 or 4 columns.
+template <typename T>
+constexpr int kColumns = 16 / (int)sizeof(T);
+template <typename T>
+struct Piece {
+  float v[kColumns<T>];
+};
+template <typename T>
+__device__ inline Piece<T> piece_of(const ds_u32x4 &bits) {
+  Piece<T> x;
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) m = fmaxf(m, x.v[k]);
+    for (int k = 0; k < 4; ++k) x.v[k] = __uint_as_float(bits[k]);
+  } else {
+    const Eight e = Elem<T>::get8(&bits, 0);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x.v[k] = e.v[k];
+  }
+  return x;
+}
+template <typename T>
+__device__ inline ds_u32x4 bits_of(const Piece<T> &x) {
+  ds_u32x4 bits;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) bits[k] = __float_as_uint(x.v[k]);
+  } else {
+    Eight e;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) e.v[k] = x.v[k];
+    Elem<T>::put8(&bits, 0, e);
+  }
+  return bits;
+}
+// Columns from j on, as many as there are up to `end`; the others are masked.
+template <typename T>
+__device__ inline Piece<T> piece_at(const T *row, int64_t j, int64_t end) {
+  if (j + kColumns<T> <= end) return piece_of<T>(*(const ds_u32x4 *)(row + j));
+  Piece<T> x;
+#pragma unroll
+  for (int k = 0; k < kColumns<T>; ++k) x.v[k] = j + k < end ? Elem<T>::get(row, j + k) : -kInf;
+  return x;
+}
+
+// Returns the piece's largest logit.
+template <typename T, bool ENTROPY>
+__device__ inline float add(Triple &a, const Piece<T> &x, float c) {
+  float peak = x.v[0];
+#pragma unroll
+  for (int k = 1; k < kColumns<T>; ++k) peak = fmaxf(peak, x.v[k]);
+  const float m = fmaxf(a.m, peak);
   raise<ENTROPY>(a, m, c);
   const float base = finite_or_0(m);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
+  for (int k = 0; k < kColumns<T>; ++k) {
     const float d = x.v[k] - base, e = __builtin_amdgcn_exp2f(d * c);
     a.s += e;
     if (ENTROPY) a.t += e * fmaxf(d, kLowest);
   }
+  return peak;
 }
 
 // Larger for a larger logit, and of equal ones for the lower column; 0 is below all.
@@ -110,13 +152,29 @@ __device__ inline void put_top(const Forward &a, int64_t i, int rank, uint64_t k
   if (a.top_logprobs) a.top_logprobs[i * a.top + rank] = bad ? __uint_as_float(0x7fc00000u) : key ? a.scale * (key_logit(key) - r.m) - logf(r.s) : -kInf;
 }
 
-__device__ inline uint64_t wave_max(uint64_t x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    const uint64_t o = __shfl_xor((unsigned long long)x, d, 64);
-    x = o > x ? o : x;
-  }
-  return x;
+// Over the wavefront, in every lane: neighbours, quads, eights, rows of 16, then rows' last lanes into the rows behind them.
+template <int CTRL, int ROWS>
+__device__ inline float moved(float x, float without) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(without), (int)__float_as_uint(x), CTRL, ROWS, 0xf, false));
+}
+__device__ inline float last_lane(float x) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63)); }
+__device__ inline float larger(float a, float b) { return a > b ? a : b; }
+__device__ inline float all_max(float x) {
+  x = larger(x, moved<0xB1, 0xf>(x, x)), x = larger(x, moved<0x4E, 0xf>(x, x)), x = larger(x, moved<0x141, 0xf>(x, x));
+  x = larger(x, moved<0x140, 0xf>(x, x)), x = larger(x, moved<0x142, 0xa>(x, x)), x = larger(x, moved<0x143, 0xc>(x, x));
+  return last_lane(x);
+}
+__device__ inline float all_sum(float x) {
+  x += moved<0xB1, 0xf>(x, 0.f), x += moved<0x4E, 0xf>(x, 0.f), x += moved<0x141, 0xf>(x, 0.f), x += moved<0x140, 0xf>(x, 0.f);
+  x += moved<0x142, 0xa>(x, 0.f), x += moved<0x143, 0xc>(x, 0.f);
+  return last_lane(x);
+}
+template <bool ENTROPY>
+__device__ inline Triple wave_triple(Triple a, float c) {
+  raise<ENTROPY>(a, all_max(a.m), c);
+  a.s = all_sum(a.s);
+  if (ENTROPY) a.t = all_sum(a.t);
+  return a;
 }
 
 template <int THREADS>
@@ -124,161 +182,205 @@ struct Room {
   Triple triples[THREADS / 64];
   float sets[64];
   uint64_t keys[kCandidates];
-  uint64_t best[THREADS / 64];
-  uint32_t count;
+  uint64_t bound;
+  uint32_t hits[kCandidates];
+  uint32_t n_hits, count;
 };
 
 // The row's triple, in every thread.
 template <int THREADS, bool ENTROPY>
 __device__ inline Triple row_triple(Triple a, float c, Triple *room) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) a = join<ENTROPY>(a, {__shfl_xor(a.m, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)}, c);
+  a = wave_triple<ENTROPY>(a, c);
   if (THREADS == 64) return a;
   if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = a;
   __syncthreads();
-  a = room[0];
-  for (int w = 1; w < THREADS / 64; ++w) a = join<ENTROPY>(a, room[w], c);
-  return a;
+  const int lane = threadIdx.x & 63;
+  a = lane < THREADS / 64 ? room[lane] : Triple{-kInf, 0.f, 0.f};
+  return wave_triple<ENTROPY>(a, c);
 }
 
-// The likeliest of the columns from `begin` to `end`, handed to put(rank, key) by one thread each; `m`: the thread's largest logit.
+// How many of `count` keys are larger.  (Eight at a time are on their way; those behind the last are 0.)
+__device__ inline int rank_of(uint64_t key, const uint64_t *keys, int count) {
+  int rank = 0;
+  for (int k = 0; k < count; k += 8)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rank += keys[k + e] > key;
+  return rank;
+}
+
+// The likeliest of `count` columns from row[0] on, handed to put(rank, key) by one thread each.  `m`: the thread's largest logit, `peaks`: its
+// pieces' (every THREADS-th); `begin`: the number of the first column.
 template <typename T, int THREADS, typename Put>
-__device__ inline void likeliest(const Forward &a, int64_t i, int64_t begin, int64_t end, float m, Room<THREADS> &room, Put put) {
-  // the sets' largest, and the `top`-th of those
-  for (int d = 1; d < THREADS / 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-  if (threadIdx.x == 0) room.count = 0;
+__device__ inline void likeliest(const T *row, int count, int64_t begin, uint32_t top, float m, const float *peaks, Room<THREADS> &room, Put put) {
+  constexpr int W = kColumns<T>;
+  const int pieces = (count + W - 1) / W;
+  // lanes in 64 sets, then sets in 8, 16 or 32
+  if (THREADS >= 256) m = larger(m, moved<0xB1, 0xf>(m, m)), m = larger(m, moved<0x4E, 0xf>(m, m));
+  if (THREADS >= 1024) m = larger(m, moved<0x141, 0xf>(m, m)), m = larger(m, moved<0x140, 0xf>(m, m));
+  if (threadIdx.x == 0) room.n_hits = room.count = 0;
   if (threadIdx.x % (THREADS / 64) == 0) room.sets[threadIdx.x / (THREADS / 64)] = m;
   __syncthreads();
-  const float set = room.sets[threadIdx.x & 63];
-  int before = 0;
-  for (int k = 0; k < 64; ++k) {
-    const float other = room.sets[k];
-    before += other > set || (other == set && k < (int)(threadIdx.x & 63));
-  }
-  const uint64_t here = __ballot(before == (int)a.top - 1);
-  const float bound = __shfl(set, __builtin_ctzll(here | 1ull << 63), 64);
-  if (m >= bound && m > -kInf) {
-    for (int64_t j = begin + threadIdx.x * 8; j < end; j += THREADS * 8) {
-      const int n = (int)(end - j < 8 ? end - j : 8);
-      const Eight x = RowsOf<T>::get(a.x, i, j, n);
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < n && x.v[k] >= bound && x.v[k] > -kInf) {
-          const uint32_t at = atomicAdd(&room.count, 1u);
-          if (at < kCandidates) room.keys[at] = key_of(x.v[k], j + k);
-        }
-    }
-  }
-  __syncthreads();
-  const uint32_t count = room.count;
-  if (count <= kCandidates) {
-    for (uint32_t at = threadIdx.x; at < count; at += THREADS) {
-      const uint64_t key = room.keys[at];
-      uint32_t rank = 0;
-      for (uint32_t k = 0; k < count; ++k) rank += room.keys[k] > key;
-      if (rank < a.top) put((int)rank, key);
-    }
-    for (uint32_t rank = count + threadIdx.x; rank < a.top; rank += THREADS) put((int)rank, 0);
-    return;
-  }
-  uint64_t last = ~0ull;
-  for (uint32_t rank = 0; rank < a.top; ++rank) {
-    uint64_t best = 0;
-    for (int64_t j = begin + threadIdx.x * 8; j < end; j += THREADS * 8) {
-      const int n = (int)(end - j < 8 ? end - j : 8);
-      const Eight x = RowsOf<T>::get(a.x, i, j, n);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint64_t key = key_of(x.v[k], j + k);
-        if (k < n && x.v[k] > -kInf && key < last && key > best) best = key;
+  float set = room.sets[threadIdx.x & 63];
+  set = larger(set, moved<0xB1, 0xf>(set, set));
+  if (top <= 16) set = larger(set, moved<0x4E, 0xf>(set, set));
+  if (top <= 8) set = larger(set, moved<0x141, 0xf>(set, set));
+  const float least = -all_max(-set);
+  uint64_t bound = least == -kInf ? 1 : key_of(least, 0xffffffff);
+  int found;
+  for (;;) {
+    // pieces that have a column that reaches the bound, or (one of them) might have
+    for (int p = threadIdx.x; p < pieces; p += THREADS) {
+      const float peak = peaks[p];
+      if (peak > -kInf && key_of(peak, begin + p * W) >= bound) {
+        const uint32_t at = atomicAdd(&room.n_hits, 1u);
+        if (at < kCandidates) room.hits[at] = p;
       }
     }
-    best = wave_max(best);
-    if (THREADS > 64) {
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) room.best[threadIdx.x >> 6] = best;
-      __syncthreads();
-      for (int w = 0; w < THREADS / 64; ++w) best = room.best[w] > best ? room.best[w] : best;
-    }
-    if (threadIdx.x == 0) put((int)rank, best);
-    last = best ? best : 1;  // behind the last there is none
-  }
-}
-
-// What is read beyond a row is masked.
-template <typename T>
-__device__ inline Eight logits_of(const typename RowsOf<T>::Bits &b, int n) {
-  Eight x = RowsOf<T>::value(b, n);
-  if (n < 8) {
+    __syncthreads();
+    const int hits = (int)room.n_hits;
+    for (int h = threadIdx.x; h < min(hits, kCandidates); h += THREADS) {
+      const int j = (int)room.hits[h] * W;
+      const Piece<T> x = piece_at(row, j, count);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x.v[k] = k < n ? x.v[k] : -kInf;
+      for (int k = 0; k < W; ++k) {
+        const uint64_t key = key_of(x.v[k], begin + j + k);
+        if (x.v[k] > -kInf && key >= bound) {
+          const uint32_t at = atomicAdd(&room.count, 1u);
+          if (at < kCandidates) room.keys[at] = key;
+        }
+      }
+    }
+    __syncthreads();
+    found = (int)room.count;
+    if (hits <= kCandidates && found <= kCandidates) break;
+    __syncthreads();
+    // a higher bound in every turn: at least kSample columns were found, no two keys are equal, and fewer are wanted
+    for (int at = threadIdx.x; at < kSample; at += THREADS)
+      if (rank_of(room.keys[at], room.keys, kSample) == (int)top - 1) room.bound = room.keys[at];
+    if (threadIdx.x == 0) room.n_hits = room.count = 0;
+    __syncthreads();
+    bound = room.bound;
   }
-  return x;
+  if (threadIdx.x < 8 && found + threadIdx.x < kCandidates) room.keys[found + threadIdx.x] = 0;
+  __syncthreads();
+  for (int at = threadIdx.x; at < found; at += THREADS) {
+    const uint64_t key = room.keys[at];
+    const int rank = rank_of(key, room.keys, found);
+    if (rank < (int)top) put(rank, key);
+  }
+  for (int rank = found + threadIdx.x; rank < (int)top; rank += THREADS) put(rank, 0);
 }
 
-// A work-group has a row, or a part of one.
-template <typename T, int THREADS, bool ENTROPY>
+// What a work-group leaves of its row, or part.
+__device__ inline void finish(const Forward &a, int64_t item, int64_t i, Triple r, int64_t token, float at) {
+  if (threadIdx.x) return;
+  if (a.parts > 1) a.triples[item] = r;
+  else put_row(a, i, r, token >= 0, at);
+}
+__device__ inline void put_likely(const Forward &a, int64_t item, int64_t i, int rank, uint64_t key, Triple r) {
+  if (a.parts == 1) put_top(a, i, rank, key, r);
+  else a.keys[item * a.top + rank] = key;
+}
+
+// A work-group has a row, or a part of one: kAhead pieces of each thread at a time, the next ones on their way.  Every load is made, so that
+// none waits for those behind it: a piece that is not whole is the last columns of a piece's size, those that others have masked.  TOP: with
+// the likeliest.
+constexpr int kAhead = 4;
+template <typename T, int THREADS, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(THREADS) void ds_logprobs_kernel(Forward a) {
-  __shared__ Room<THREADS> room;
-  constexpr int kAhead = 4;
+  __shared__ std::conditional_t<TOP, Room<THREADS>, Triple[THREADS / 64]> room;
+  extern __shared__ float peaks[];  // TOP: one for each piece
+  Triple *triples = (Triple *)&room;
+  constexpr int W = kColumns<T>, kStep = kAhead * THREADS * W;
   const float c = a.scale * kLog2e;
   for (int64_t item = blockIdx.x; item < a.rows * a.parts; item += gridDim.x) {
     const int64_t i = a.parts == 1 ? item : item / a.parts, part = item - i * a.parts;
     const int64_t begin = part * a.part_cols, end = begin + a.part_cols < a.cols ? begin + a.part_cols : a.cols;
+    const int count = (int)(end - begin), at = threadIdx.x * W;
+    const T *row = (const T *)a.x.base + i * a.x.stride + begin;
     Triple r = {-kInf, 0.f, 0.f};
-    for (int64_t first = begin; first < end; first += kAhead * THREADS * 8) {
-      typename RowsOf<T>::Bits bits[kAhead];
-      int n[kAhead];
+    const int64_t token = a.parts == 1 && threadIdx.x == 0 ? token_of(a, i) : -1;
+    if (count >= W) {
+      ds_u32x4 bits[kAhead], next[kAhead];
+      const auto ask = [&](int first, ds_u32x4 *to) {
 #pragma unroll
-      for (int e = 0; e < kAhead; ++e) {
-        const int64_t j = first + (e * THREADS + threadIdx.x) * 8, left = end - j;
-        n[e] = (int)(left < 0 ? 0 : left < 8 ? left : 8);
-        bits[e] = RowsOf<T>::ask(a.x, i, j, n[e]);
-      }
+        for (int e = 0; e < kAhead; ++e) to[e] = *(const ds_u32x4 *)(row + min(first + e * THREADS * W + at, count - W));
+      };
+      ask(0, bits);
+      for (int first = 0;;) {
+        const int left = count - first;
+        ask(left > kStep ? first + kStep : first, next);
+        if (left >= kStep) {
 #pragma unroll
-      for (int e = 0; e < kAhead; ++e)
-        if (n[e] > 0) add8<ENTROPY>(r, logits_of<T>(bits[e], n[e]), c);
-    }
-    const float m = r.m;
-    r = row_triple<THREADS, ENTROPY>(r, c, room.triples);
-    if (a.parts == 1) {
-      if (threadIdx.x == 0) {
-        const int64_t token = token_of(a, i);
-        put_row(a, i, r, token >= 0, token >= 0 ? Elem<T>::get(a.x.base, i * a.x.stride + token) : 0.f);
+          for (int e = 0; e < kAhead; ++e) {
+            const float peak = add<T, ENTROPY>(r, piece_of<T>(bits[e]), c);
+            if (TOP) peaks[first / W + e * THREADS + threadIdx.x] = peak;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < kAhead; ++e) {
+            const int shift = e * THREADS * W + at - (left - W);
+            if (shift >= W) break;
+            Piece<T> x = piece_of<T>(bits[e]);
+#pragma unroll
+            for (int k = 0; k < W; ++k) x.v[k] = k >= shift ? x.v[k] : -kInf;
+            const float peak = add<T, ENTROPY>(r, x, c);
+            if (TOP) peaks[first / W + e * THREADS + threadIdx.x] = peak;
+          }
+        }
+        if (left <= kStep) break;
+        first += kStep;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) bits[e] = next[e];
       }
-      if (a.top) likeliest<T, THREADS>(a, i, begin, end, m, room, [&](int rank, uint64_t key) { put_top(a, i, rank, key, r); });
-    } else {
-      if (threadIdx.x == 0) a.triples[item] = r;
-      if (a.top) likeliest<T, THREADS>(a, i, begin, end, m, room, [&](int rank, uint64_t key) { a.keys[item * a.top + rank] = key; });
+    } else if (at < count) {
+      const float peak = add<T, ENTROPY>(r, piece_at(row, at, count), c);
+      if (TOP) peaks[threadIdx.x] = peak;
     }
-    if (THREADS > 64 || a.top) __syncthreads();
+    const float m = r.m, given = token >= 0 ? Elem<T>::get(row, token) : 0.f;
+    r = row_triple<THREADS, ENTROPY>(r, c, triples);
+    finish(a, item, i, r, token, given);
+    if constexpr (TOP)
+      likeliest<T, THREADS>(row, count, begin, a.top, m, peaks, room, [&](int rank, uint64_t key) { put_likely(a, item, i, rank, key, r); });
+    if (THREADS > 64 || TOP) __syncthreads();
   }
 }
 
-// The parts of a row joined: a work-group has a row.
+// The parts of a row joined: a work-group has a row.  Its likeliest so far, and as many of the parts' as there are threads left, are ranked
+// until all have been.
+constexpr int kMostKeys = 256 - (int)DS_TOP_MOST;
 template <typename T, bool ENTROPY>
 __global__ __launch_bounds__(256) void ds_logprobs_join_kernel(Forward a) {
-  __shared__ uint64_t keys[kCandidates];
+  __shared__ uint64_t keys[256], best[DS_TOP_MOST];
   const float c = a.scale * kLog2e;
   for (int64_t i = blockIdx.x; i < a.rows; i += gridDim.x) {
-    Triple r = a.triples[i * a.parts];
-    for (int p = 1; p < a.parts; ++p) r = join<ENTROPY>(r, a.triples[i * a.parts + p], c);
-    if (threadIdx.x == 0) {
-      const int64_t token = token_of(a, i);
-      put_row(a, i, r, token >= 0, token >= 0 ? Elem<T>::get(a.x.base, i * a.x.stride + token) : 0.f);
+    const int lane = threadIdx.x & 63, spare = threadIdx.x - (int)DS_TOP_MOST;
+    const int64_t token = token_of(a, i), count = (int64_t)a.parts * a.top;
+    const float at = token >= 0 ? Elem<T>::get(a.x.base, i * a.x.stride + token) : 0.f;
+    uint64_t key = spare >= 0 && spare < count ? a.keys[i * count + spare] : 0;
+    Triple r = {-kInf, 0.f, 0.f};
+    for (int p = lane; p < a.parts; p += 64) {
+      Triple o = a.triples[i * a.parts + p];
+      const float m = fmaxf(r.m, o.m);
+      raise<ENTROPY>(r, m, c), raise<ENTROPY>(o, m, c);
+      r.s += o.s, r.t += o.t;
     }
+    r = wave_triple<ENTROPY>(r, c);
+    if (threadIdx.x == 0) put_row(a, i, r, token >= 0, at);
     if (!a.top) continue;
-    const int count = a.parts * (int)a.top;
-    __syncthreads();
-    for (int k = threadIdx.x; k < count; k += 256) keys[k] = a.keys[i * count + k];
-    __syncthreads();
-    // (keys of 0, of parts that have fewer, are behind all others in the order of their place)
-    for (int at = threadIdx.x; at < count; at += 256) {
-      const uint64_t key = keys[at];
-      int rank = 0;
-      for (int k = 0; k < count; ++k) rank += keys[k] > key || (keys[k] == key && k < at);
-      if (rank < (int)a.top) put_top(a, i, rank, key, r);
+    for (int64_t first = 0; first < count; first += kMostKeys) {
+      __syncthreads();
+      if (spare < 0) key = first ? best[threadIdx.x] : 0;
+      else if (first) key = first + spare < count ? a.keys[i * count + first + spare] : 0;
+      keys[threadIdx.x] = key;
+      __syncthreads();
+      if (spare < 0) best[threadIdx.x] = 0;
+      __syncthreads();
+      const int rank = key ? rank_of(key, keys, 256) : 256;
+      if (rank < (int)a.top) best[rank] = key;
     }
+    __syncthreads();
+    if (threadIdx.x < a.top) put_top(a, i, threadIdx.x, best[threadIdx.x], r);
   }
 }
 
@@ -291,53 +393,84 @@ struct Backward {
   uint32_t across;  // work-groups of a row
 };
 
-// A work-group has kPiecesEach * 256 pieces of eight columns of a row.
+// A work-group has kPiecesEach * 256 pieces of a row.  (Loads as above.)
 constexpr int kPiecesEach = 4;
-template <typename T>
+template <typename T, bool ENTROPY, bool STREAM>
 __global__ __launch_bounds__(256) void ds_logprobs_backward_kernel(Backward a) {
+  constexpr int W = kColumns<T>, kStep = kPiecesEach * 256 * W;
   for (int64_t item = blockIdx.x; item < a.rows * a.across; item += gridDim.x) {
-    const int64_t i = item / a.across, first = (item - i * a.across) * (kPiecesEach * 256 * 8);
-    typename RowsOf<T>::Bits bits[kPiecesEach];
-    int n[kPiecesEach];
+    const int64_t i = item / a.across, first = (item - i * a.across) * kStep;
+    const int left = (int)(a.cols - first < kStep ? a.cols - first : kStep), at = threadIdx.x * W;
+    const T *row = (const T *)a.x.base + i * a.x.stride + first;
+    T *to = (T *)a.dx.base + i * a.dx.stride + first;
+    // (a piece before the row's end, which may begin before `first`; or, in a row shorter than a piece, none)
+    const bool pieces = a.cols >= W;
+    ds_u32x4 bits[kPiecesEach] = {};
+    if (pieces) {
 #pragma unroll
-    for (int e = 0; e < kPiecesEach; ++e) {
-      const int64_t j = first + (e * 256 + threadIdx.x) * 8, left = a.cols - j;
-      n[e] = (int)(left < 0 ? 0 : left < 8 ? left : 8);
-      bits[e] = RowsOf<T>::ask(a.x, i, j, n[e]);
+      for (int e = 0; e < kPiecesEach; ++e) {
+        const ds_u32x4 *from = (const ds_u32x4 *)(row + min(e * 256 * W + at, left - W));
+        bits[e] = STREAM ? __builtin_nontemporal_load(from) : *from;
+      }
     }
     const int64_t token = a.tokens ? a.tokens[i] : -1;
     const bool given = token >= 0 && token < a.cols;
-    const float up = given && a.dlogprob ? a.dlogprob[i] * a.scale : 0.f, along = a.dentropy ? a.dentropy[i] * a.scale : 0.f;
-    const float m = a.largest[i], logsum = a.logsum[i], h = a.dentropy ? a.entropy[i] : 0.f;
+    const float up = given && a.dlogprob ? a.dlogprob[i] * a.scale : 0.f, along = ENTROPY ? a.dentropy[i] * a.scale : 0.f;
+    const float m = a.largest[i], logsum = a.logsum[i], h = ENTROPY ? a.entropy[i] : 0.f;
     const bool zero = m == -kInf || (up == 0.f && along == 0.f);
+    const float c = a.scale * kLog2e, o = logsum * kLog2e;
 #pragma unroll
     for (int e = 0; e < kPiecesEach; ++e) {
-      const int64_t j = first + (e * 256 + threadIdx.x) * 8;
-      Eight x = RowsOf<T>::value(bits[e], n[e]);
+      const int j = e * 256 * W + at, shift = j - (left - W);
+      if (left < kStep && j >= left) break;
+      Piece<T> x = {};
+      if (!zero) {
+        x = pieces ? piece_of<T>(bits[e]) : piece_at(row, j, left);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float logp = a.scale * (x.v[k] - m) - logsum, p = __builtin_amdgcn_exp2f(logp * kLog2e);
-        float d = p == 0.f ? 0.f : -p * (up + along * (logp + h));
-        if (given && j + k == token) d += up;
-        x.v[k] = zero ? 0.f : d;
+        for (int k = 0; k < W; ++k) {
+          const float z = x.v[k] - m, p = __builtin_amdgcn_exp2f(__builtin_fmaf(z, c, -o));
+          x.v[k] = ENTROPY ? (p == 0.f ? 0.f : -p * (up + along * (__builtin_fmaf(z, a.scale, -logsum) + h))) : -p * up;
+        }
+        const int64_t column = token - first - (pieces ? min(j, left - W) : j);
+        if (given && column >= 0 && column < W) {
+#pragma unroll
+          for (int k = 0; k < W; ++k) x.v[k] += column == k ? up : 0.f;
+        }
       }
-      put_up_to8<T>(a.dx.base, i * a.dx.stride + j, n[e], x);
+      if (pieces && shift <= 0) {
+        const ds_u32x4 o = bits_of<T>(x);
+        if (STREAM) __builtin_nontemporal_store(o, (ds_u32x4 *)(to + j));
+        else *(ds_u32x4 *)(to + j) = o;
+      } else {
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          const int column = pieces ? left - W + k : j + k;
+          if (column >= j && column < left) Elem<T>::put(to, column, x.v[k]);
+        }
+      }
     }
   }
 }
 
-// Parts of a row, where few rows leave most of the card idle: so many that the work-groups are about as many as the CUs, each of at least
-// kLeast columns; and no more candidates than the kernel that joins them has room for.
-constexpr int64_t kLeast = 8192;
-int64_t parts_of(int64_t rows, int64_t cols, uint32_t top) {
-  if (rows <= 0 || rows > 128) return 1;
-  int64_t parts = std::min((256 + rows - 1) / rows, (cols + kLeast - 1) / kLeast);
-  if (top) parts = std::min<int64_t>(parts, kCandidates / top);
-  return std::max<int64_t>(1, std::min<int64_t>(parts, 64));
+// Bytes of a gradient from which on it is not to stay in the caches.
+constexpr int64_t kStream = 64 << 20;
+
+// Parts of a row: where few rows leave most of the card idle, so many that the work-groups are about as many as the CUs, each of at least
+// kLeast columns, and no more candidates than the kernel that joins them has threads; but as many as it takes where the likeliest are looked for.
+constexpr int64_t kLeast = 32768;
+int64_t part_cols_of(int64_t cols, int64_t parts) { return ((cols + parts - 1) / parts + 7) / 8 * 8; }
+int64_t parts_of(int64_t rows, int64_t cols, uint32_t top, int64_t size) {
+  int64_t parts = 1;
+  if (rows <= 128) {
+    parts = std::min((256 + rows - 1) / rows, (cols + kLeast - 1) / kLeast);
+    if (top) parts = std::min<int64_t>(parts, kMostKeys / top);
+    parts = std::min<int64_t>(parts, 64);
+  }
+  const int64_t most = kMostPieces * 16 / size;
+  return std::max(parts, top ? (cols + most - 1) / most : 1);
 }
 
-uint64_t workspace_of(int64_t rows, int64_t cols, uint32_t top) {
-  const int64_t parts = parts_of(rows, cols, top);
+uint64_t workspace_of(int64_t rows, int64_t parts, uint32_t top) {
   if (parts == 1) return 0;
   return (uint64_t)(((rows * parts * (int64_t)sizeof(Triple) + 15) & ~15ll) + rows * parts * top * 8);
 }
@@ -354,7 +487,11 @@ bool is_scale(float s) { return s > 0.f && s < kInf; }
 extern "C" int ds_logprobs_workspace(const ds_matrix *logits, uint32_t top, uint64_t *bytes) {
   DS_TRY(check_logits(logits));
   if (!bytes || top > DS_TOP_MOST) return DS_EINVAL;
-  *bytes = logits->cols ? workspace_of(logits->rows, logits->cols, top) : 0;
+  const int64_t rows = logits->rows, cols = logits->cols, size = ds_itemsize(logits->dtype);
+  *bytes = 0;
+  // (enough for a call without the likeliest too)
+  if (rows && cols)
+    *bytes = std::max(workspace_of(rows, parts_of(rows, cols, top, size), top), workspace_of(rows, parts_of(rows, cols, 0, size), 0));
   return DS_OK;
 }
 
@@ -369,27 +506,32 @@ extern "C" int ds_logprobs(const ds_matrix *logits, float scale, const int64_t *
   const int64_t rows = logits->rows, cols = logits->cols;
   if (rows == 0) return DS_OK;
   if (!top_tokens && !top_logprobs) top = 0;
-  const int64_t parts = cols ? parts_of(rows, cols, top) : 1;
+  const int64_t parts = cols ? parts_of(rows, cols, top, ds_itemsize(logits->dtype)) : 1;
   if (parts > 1) {
     if (!workspace || ds_misaligned(workspace, 16)) return DS_EINVAL;
-    if (workspace_bytes < workspace_of(rows, cols, top)) return DS_ERANGE;
+    if (workspace_bytes < workspace_of(rows, parts, top)) return DS_ERANGE;
   }
-  const int64_t keys_at = (rows * parts * (int64_t)sizeof(Triple) + 15) & ~15ll, part_cols = ((cols + parts - 1) / parts + 7) / 8 * 8;
+  const int64_t keys_at = (rows * parts * (int64_t)sizeof(Triple) + 15) & ~15ll, part_cols = part_cols_of(cols, parts);
   const Forward a{ds_rows(logits), tokens, logprob, largest, logsum, entropy, top_tokens, top_logprobs, rows, cols, scale, top, part_cols,
                   (int32_t)parts, (Triple *)workspace, (uint64_t *)((uint8_t *)workspace + keys_at)};
   return ds_with_type(logits->dtype, [&](auto type) -> int {
     typedef decltype(type) T;
     const auto with = [&](auto wanted) -> int {
       constexpr bool E = decltype(wanted)::value;
-      const auto launch = [&](auto kernel, int threads, int64_t groups) -> int {
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(groups, kMaxGrid)), dim3(threads), 0, (hipStream_t)stream, a);
+      const int64_t pieces = top ? (part_cols + kColumns<T> - 1) / kColumns<T> : 0;
+      const auto launch = [&](auto kernel, int threads, int64_t groups, int64_t floats) -> int {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(groups, kMaxGrid)), dim3(threads), (uint32_t)(floats * 4), (hipStream_t)stream, a);
         DS_HIP_TRY(hipGetLastError());
         return DS_OK;
       };
-      if (parts == 1 && cols <= 2048) return launch(ds_logprobs_kernel<T, 64, E>, 64, rows);
-      if (parts == 1 && rows > 256) return launch(ds_logprobs_kernel<T, 256, E>, 256, rows);
-      DS_TRY(launch(ds_logprobs_kernel<T, 1024, E>, 1024, rows * parts));
-      return parts == 1 ? DS_OK : launch(ds_logprobs_join_kernel<T, E>, 256, rows);
+      const auto rows_with = [&](auto likeliest) -> int {
+        constexpr bool TOP = decltype(likeliest)::value;
+        if (cols <= 2048) return launch(ds_logprobs_kernel<T, 64, E, TOP>, 64, rows, pieces);
+        if (rows * parts > 256) return launch(ds_logprobs_kernel<T, 256, E, TOP>, 256, rows * parts, pieces);
+        return launch(ds_logprobs_kernel<T, 1024, E, TOP>, 1024, rows * parts, pieces);
+      };
+      DS_TRY(top ? rows_with(std::true_type()) : rows_with(std::false_type()));
+      return parts == 1 ? DS_OK : launch(ds_logprobs_join_kernel<T, E>, 256, rows, 0);
     };
     return entropy ? with(std::true_type()) : with(std::false_type());
   });
@@ -405,12 +547,18 @@ extern "C" int ds_logprobs_backward(const ds_matrix *logits, float scale, const 
     return DS_EINVAL;
   if (logits->rows == 0 || logits->cols == 0) return DS_OK;
   if (!largest || !logsum) return DS_EINVAL;
-  const uint32_t across = (uint32_t)((logits->cols + kPiecesEach * 2048 - 1) / (kPiecesEach * 2048));
+  const int64_t size = ds_itemsize(logits->dtype), step = kPiecesEach * 256 * 16 / size;
+  const uint32_t across = (uint32_t)((logits->cols + step - 1) / step);
+  const bool stream_it = logits->rows * logits->cols >= kStream / size;
   const Backward a{ds_rows(logits), ds_rows(dlogits), tokens, largest, logsum, entropy, dlogprob, dentropy, logits->rows, logits->cols, scale, across};
   return ds_with_type(logits->dtype, [&](auto type) -> int {
     typedef decltype(type) T;
-    hipLaunchKernelGGL(ds_logprobs_backward_kernel<T>, dim3((uint32_t)std::min(a.rows * across, kMaxGrid)), dim3(256), 0, (hipStream_t)stream, a);
-    DS_HIP_TRY(hipGetLastError());
-    return DS_OK;
+    const auto launch = [&](auto kernel) -> int {
+      hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(a.rows * across, kMaxGrid)), dim3(256), 0, (hipStream_t)stream, a);
+      DS_HIP_TRY(hipGetLastError());
+      return DS_OK;
+    };
+    if (dentropy) return stream_it ? launch(ds_logprobs_backward_kernel<T, true, true>) : launch(ds_logprobs_backward_kernel<T, true, false>);
+    return stream_it ? launch(ds_logprobs_backward_kernel<T, false, true>) : launch(ds_logprobs_backward_kernel<T, false, false>);
   });
 }

@@ -357,7 +357,7 @@ def logits(rng, rows, cols, masked=0.0):
 
 
 LP_SIZES = [(1, 1), (3, 2), (5, 9), (2, 63), (4, 512), (300, 513), (2, 2047), (3, 2048), (3, 2049), (300, 2100), (2, 8191), (5, 8193), (1, 32000),
-            (260, 16400), (1, 70001), (130, 16390)]
+            (260, 16400), (1, 70001), (130, 16390), (3, 150001)]
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -373,7 +373,7 @@ def test_logprobs(rows, cols, kind):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("cols", [40, 3000, 9000, 40000])
+@pytest.mark.parametrize("cols", [40, 3000, 9000, 40000, 100000])
 def test_logprobs_of_ties(cols, kind):
     """Equal logits: the lowest columns first, however many there are."""
     rng = np.random.default_rng(cols)
@@ -383,6 +383,16 @@ def test_logprobs_of_ties(cols, kind):
     x[3, cols // 2:] = -np.inf
     for rows in (4, 300):
         check_probabilities(np.tile(x, (rows // 4, 1)), kind, np.zeros(rows, np.int64), 1.0, 32)
+
+
+@pytest.mark.parametrize("cols", [300, 3000, 33000, 100000])
+def test_logprobs_of_rows_in_order(cols):
+    """The likeliest next to each other, where one thread reads them: first, last, in the middle."""
+    x = np.linspace(5, -5, cols)
+    rows = np.stack([x, x[::-1], np.roll(x, cols // 2), np.floor(x), np.floor(x)[::-1]])
+    for kind in ("f32", "bf16"):
+        for times in (1, 60):
+            check_probabilities(np.tile(rows, (times, 1)), kind, np.zeros(5 * times, np.int64), 1.0, 32)
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -748,7 +758,7 @@ def test_moments_in_8_bits_are_rounded_without_a_bias():
 def everything(seed):
     """A pass of all operators on inputs of a seed, as a function that can be called again, and the tensors that it writes."""
     rng = np.random.default_rng(seed)
-    rows, cols, vocab = 70, 640, 20000
+    rows, cols, vocab = 70, 640, 100000
     j = Joint(rng, cols, "bf16", True, True, True)
     u, x, out, y, dout, dy, du, dx = (Mat(hidden(rng, rows, cols), "bf16") for _ in range(8))
     ra, rb, sums = floats(rows)[0], floats(rows)[0], [floats(cols)[0] for _ in range(3)]
