@@ -270,11 +270,12 @@ def test_log_probabilities_of_nothing():
 def test_log_probability_workspaces(top):
     assert ds.ds_logprobs_workspace(mat(0, 100), top) == 0 and ds.ds_logprobs_workspace(mat(4, 0), top) == 0
     assert ds.ds_logprobs_workspace(mat(1, 1), top) == 0 and ds.ds_logprobs_workspace(mat(100000, 32000), top) == 0
+    # a row in parts, each of which leaves three floats and its likeliest: at most 64 of them, or one for every 2^16 columns of 16 bits
     need = ds.ds_logprobs_workspace(mat(1, 1 << 30), top)
-    assert 0 < need <= 64 * 12 + 16 + 1024 * 8                       # at most 64 parts, and 1024 candidates of a row
+    assert 0 < need <= max(64, (1 << 14) if top else 0) * (12 + 8 * top) + 16
     # what is asked for the likeliest is enough for a call that leaves them out
-    for rows, cols in ((1, 32000), (3, 150000), (64, 100000)):
-        assert ds.ds_logprobs_workspace(mat(rows, cols), top) >= ds.ds_logprobs_workspace(mat(rows, cols), 0) * (top == 0)
+    for rows, cols in ((1, 32000), (3, 150000), (64, 100000), (1000, 300000), (1, 1 << 30)):
+        assert ds.ds_logprobs_workspace(mat(rows, cols), top) >= ds.ds_logprobs_workspace(mat(rows, cols), 0)
 
 
 def entry(param=None, grad=None, m=None, v=None, copy=0, decay=0.1, rate=1.0, at=PTR, eight=False):
