@@ -48,6 +48,15 @@ __device__ inline Eight weight_of(const Vectors &v, int64_t j, int n) {
   return w;
 }
 
+// Waits for loads here, where what was asked for behind them is known: at the head of a loop the compiler would wait for all.
+template <typename B>
+__device__ inline void arrived(B &bits) {
+#pragma unroll
+  for (int q = 0; q < (int)(sizeof(B) / 16); ++q)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(bits.w[q][k]));
+}
+
 // What eight elements of out are when they are read back.
 template <typename T>
 __device__ inline void as_stored(Eight &e) {
@@ -64,54 +73,76 @@ struct JoinForward {
   bool after, before;
 };
 
-// WAVES wavefronts have a row, each thread HAS pieces of eight columns, 512 * WAVES apart; a work-group of WIDE wavefronts has
-// WIDE / WAVES rows at a time.  AHEAD: it asks for the next row before it computes on this one, where the registers hold both.
-template <typename T, int WAVES, int WIDE, int HAS, bool AHEAD = true>
+// The sum of a row's `WAVES` wavefronts, the which-th of the work-group, in every thread.  `room`: a float for each wavefront, another one in
+// every turn: it is written again only behind the barrier of a sum in between.
+template <int WAVES>
+__device__ inline float total_of_row(float x, float *room, int which) {
+  x = all_sum(x);
+  if (WAVES == 1) return x;
+  if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = room[which * WAVES + threadIdx.x % WAVES];
+  x += moved<0xB1, 0xf>(x, 0.f);
+  if (WAVES >= 4) x += moved<0x4E, 0xf>(x, 0.f);
+  if (WAVES >= 8) x += moved<0x141, 0xf>(x, 0.f);
+  if (WAVES >= 16) x += moved<0x140, 0xf>(x, 0.f);
+  return x;
+}
+
+// WAVES wavefronts have a row, each thread HAS pieces of it, 512 * WAVES columns apart; a work-group of WIDE wavefronts has WIDE / WAVES rows at a
+// time, and the next ones on their way.  The compiler counts what is on its way only where nothing is conditional, and waits for all of it,
+// the last row's stores too, elsewhere.  So, from a row of a piece on (PIECES), every load and store is made: a piece that is not whole is the row's
+// last eight columns, left out of the sums where others have them, but computed and stored as they do; rows beyond the last are the last;
+// without a block x is read for u.  Nothing is stored before the whole row has been read: out may be x.
+template <typename T, int WAVES, int WIDE, int HAS, bool PIECES>
 __global__ __launch_bounds__(WIDE * 64) void ds_join_forward_kernel(JoinForward a) {
   __shared__ float room[2][2][WIDE];
   constexpr int kRows = WIDE / WAVES, kApart = WAVES * 512;
-  const int at = threadIdx.x % (WAVES * 64) * 8, which = threadIdx.x / (WAVES * 64);
+  const int at = threadIdx.x % (WAVES * 64) * 8, which = kRows == 1 ? 0 : threadIdx.x / (WAVES * 64);
   const bool joins = a.u.base != nullptr;
+  const Rows u_or_x = joins ? a.u : a.x;
   const float each = 1.f / (float)a.cols;
   const int64_t stride = (int64_t)gridDim.x * kRows;
-  int64_t i = (int64_t)blockIdx.x * kRows + which;
-  int n[HAS];
-  typename RowsOf<T>::Bits next_x[HAS], next_u[HAS] = {};
-  const auto ask = [&](int64_t i) {
-#pragma unroll
-    for (int p = 0; p < HAS; ++p) {
-      const int has = i < a.rows ? n[p] : 0;
-      next_x[p] = RowsOf<T>::ask(a.x, i, at + p * kApart, has);
-      if (joins) next_u[p] = RowsOf<T>::ask(a.u, i, at + p * kApart, has);
-    }
-  };
-#pragma unroll
-  for (int p = 0; p < HAS; ++p) n[p] = columns_left(a.cols, at + p * kApart);
-  if (AHEAD) ask(i);
+  int n[HAS], from[HAS], others[HAS];
   Eight w[HAS], g[HAS];
 #pragma unroll
   for (int p = 0; p < HAS; ++p) {
-    w[p] = weight_of(a.v, at + p * kApart, n[p]);
-    g[p] = get_up_to8_any(a.v.before_gamma, a.v.dtype, at + p * kApart, n[p], 1.f);
+    const int j = at + p * kApart;
+    n[p] = columns_left(a.cols, j);
+    from[p] = PIECES && n[p] < 8 ? (int)a.cols - 8 : j, others[p] = j - from[p];
+    w[p] = weight_of(a.v, from[p], PIECES ? 8 : n[p]);
+    g[p] = get_up_to8_any(a.v.before_gamma, a.v.dtype, from[p], PIECES ? 8 : n[p], 1.f);
   }
+  typedef typename RowsOf<T>::Bits Bits;
+  Bits next_x[HAS], next_u[HAS];
+  const auto ask = [&](int64_t i) {
+    const int64_t there = i < a.rows ? i : a.rows - 1;
+#pragma unroll
+    for (int p = 0; p < HAS; ++p)
+      next_x[p] = RowsOf<T>::ask(a.x, there, from[p], PIECES ? 8 : n[p]), next_u[p] = RowsOf<T>::ask(u_or_x, there, from[p], PIECES ? 8 : n[p]);
+  };
+  const auto put = [&](const Rows &to, int64_t i, int p, const Eight &x) {
+    const int64_t there = i < a.rows ? i : a.rows - 1;
+    if (PIECES) Elem<T>::put8(to.base, there * to.stride + from[p], x);
+    else put_up_to8<T>(to.base, there * to.stride + from[p], n[p], x);
+  };
+  constexpr bool kAhead = sizeof(T) == 2 || HAS == 1;  // where the registers hold both rows
+  int64_t i = (int64_t)blockIdx.x * kRows + which;
+  if (kAhead) ask(i);
   int turn = 0;
   for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.rows; first += stride, i += stride, turn ^= 1) {
+    if (!kAhead) ask(i);
     Eight x[HAS], u[HAS];
     float squares = 0.f;
-    if (!AHEAD) ask(i);
 #pragma unroll
     for (int p = 0; p < HAS; ++p) {
-      x[p] = RowsOf<T>::value(next_x[p], n[p]), u[p] = RowsOf<T>::value(next_u[p], n[p]);
+      x[p] = RowsOf<T>::value(next_x[p], 8), u[p] = RowsOf<T>::value(next_u[p], 8);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) squares += u[p].v[k] * u[p].v[k];
+      for (int k = 0; k < 8; ++k) squares += k >= others[p] ? u[p].v[k] * u[p].v[k] : 0.f;
     }
-    if (AHEAD) ask(i + stride);
-    const bool row = i < a.rows;
+    if (kAhead) ask(first + stride < a.rows ? i + stride : i);
     float after = 1.f;
-    if (a.after) {
-      after = 1.f / sqrtf(row_sum<WAVES>(squares, room[turn][0]) * each + a.v.eps);
-      if (row && at == 0 && a.rstd_after) a.rstd_after[i] = after;
-    }
+    if (a.after) after = 1.f / sqrtf(total_of_row<WAVES>(squares, room[turn][0], which) * each + a.v.eps);
     squares = 0.f;
 #pragma unroll
     for (int p = 0; p < HAS; ++p) {
@@ -119,20 +150,27 @@ __global__ __launch_bounds__(WIDE * 64) void ds_join_forward_kernel(JoinForward 
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[p].v[k] = a.v.keep * x[p].v[k] + u[p].v[k] * after * w[p].v[k];
         as_stored<T>(x[p]);
-        if (row && a.out.base) put_up_to8<T>(a.out.base, i * a.out.stride + at + p * kApart, n[p], x[p]);
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) squares += k < n[p] ? x[p].v[k] * x[p].v[k] : 0.f;
+      for (int k = 0; k < 8; ++k) squares += k >= others[p] ? x[p].v[k] * x[p].v[k] : 0.f;
     }
-    if (!a.before) continue;
-    const float before = 1.f / sqrtf(row_sum<WAVES>(squares, room[turn][1]) * each + a.v.eps);
-    if (!row) continue;
-    if (at == 0 && a.rstd_before) a.rstd_before[i] = before;
+    const float before = 1.f / sqrtf(total_of_row<WAVES>(squares, room[turn][1], which) * each + a.v.eps);
+    if (WAVES == 1) __syncthreads();
+    if (at == 0 && i < a.rows) {
+      if (a.after && a.rstd_after) a.rstd_after[i] = after;
+      if (a.before && a.rstd_before) a.rstd_before[i] = before;
+    }
 #pragma unroll
     for (int p = 0; p < HAS; ++p) {
+      if (joins) put(a.out, i, p, x[p]);
+      if (!a.before) continue;
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[p].v[k] = x[p].v[k] * before * g[p].v[k];
-      put_up_to8<T>(a.y.base, i * a.y.stride + at + p * kApart, n[p], x[p]);
+      put(a.y, i, p, x[p]);
+    }
+    if (kAhead) {
+#pragma unroll
+      for (int p = 0; p < HAS; ++p) arrived(next_x[p]), arrived(next_u[p]);
     }
   }
 }
@@ -193,101 +231,126 @@ struct JoinBackward {
   bool after, before;
 };
 
-// The shapes are the forward kernel's.
-template <typename T, int WAVES, int WIDE, int HAS>
+// WAVES wavefronts have a row, each thread a piece of it; a work-group of WIDE wavefronts has WIDE / WAVES rows at a time, and the next ones on
+// their way.  The norms' sums are taken together: with A = sum g h / cols,
+//   sum w k = sum (scale gate after_gamma) k (dout + rstd_before g) - rstd_before A sum (scale gate after_gamma) k h.
+// The compiler counts what is on its way only where nothing is conditional, and waits for all of it, the last row's stores too, elsewhere.  So, from
+// a row of a piece on (PIECES), every load and store is made: a piece that is not whole is the row's last eight columns, left out of the
+// sums where others have them, but computed and stored as they do; rows beyond the last are the last; what there is none of is read from
+// where there is something.  WHOLE: all pieces are whole and the threads' own.  BOTH: du and dx are wanted.
+template <typename T, int WAVES, int WIDE, bool PIECES, bool WHOLE, bool BOTH>
 __global__ __launch_bounds__(WIDE * 64) void ds_join_backward_kernel(JoinBackward a) {
   constexpr int kRows = WIDE / WAVES, kApart = WAVES * 512;
-  __shared__ float room[2][2][WIDE];
-  __shared__ float lines[kRows > 1 ? kRows : 1][kRows > 1 ? HAS * kApart : 1];
-  const int at = threadIdx.x % (WAVES * 64) * 8, which = threadIdx.x / (WAVES * 64);
+  __shared__ float room[2][3][WIDE];
+  __shared__ float lines[kRows > 1 ? kRows : 1][kRows > 1 ? kApart : 1];
+  const int at = threadIdx.x % (WAVES * 64) * 8, which = kRows == 1 ? 0 : threadIdx.x / (WAVES * 64);
   const bool joins = a.u.base != nullptr;
+  JoinBackward s = a;
+  if (PIECES) {
+    const Rows some = a.before ? a.dy : a.dout;
+    if (!a.dout.base) s.dout = some;
+    if (!a.before) s.dy = s.out = some, s.rstd_before = (const float *)some.base;
+    if (!joins) s.u = some;
+    if (!a.after) s.rstd_after = (const float *)some.base;
+  }
   const float each = 1.f / (float)a.cols;
   const int64_t stride = (int64_t)gridDim.x * kRows;
-  Eight g[HAS], w[HAS], da[HAS] = {}, db[HAS] = {};
-  int n[HAS];
-#pragma unroll
-  for (int p = 0; p < HAS; ++p) {
-    n[p] = columns_left(a.cols, at + p * kApart);
-    g[p] = get_up_to8_any(a.v.before_gamma, a.v.dtype, at + p * kApart, n[p], 1.f);
-    w[p] = weight_of(a.v, at + p * kApart, n[p]);
-  }
+  const int n = WHOLE ? 8 : columns_left(a.cols, at);
+  const int from = PIECES && n < 8 ? (int)a.cols - 8 : at, others = at - from;  // the first column, and how many are others'
+  const Eight g = get_up_to8_any(a.v.before_gamma, a.v.dtype, from, PIECES ? 8 : n, 1.f), w = weight_of(a.v, from, PIECES ? 8 : n);
+  Eight da = {}, db = {};
+  struct Row {
+    typename RowsOf<T>::Bits d, u, y, o;
+    float before, after;
+  };
+  const auto ask = [&](Row &r, int64_t i) {
+    const int64_t there = i < a.rows ? i : a.rows - 1;
+    if (PIECES) {
+      r.d = RowsOf<T>::ask(s.dout, there, from, 8), r.u = RowsOf<T>::ask(s.u, there, from, 8);
+      r.y = RowsOf<T>::ask(s.dy, there, from, 8), r.o = RowsOf<T>::ask(s.out, there, from, 8);
+      r.before = s.rstd_before[there], r.after = s.rstd_after[there];
+      return;
+    }
+    r = Row{};
+    if (a.dout.base) r.d = RowsOf<T>::ask(a.dout, there, from, n);
+    if (a.before) r.y = RowsOf<T>::ask(a.dy, there, from, n), r.o = RowsOf<T>::ask(a.out, there, from, n), r.before = a.rstd_before[there];
+    if (joins) r.u = RowsOf<T>::ask(a.u, there, from, n);
+    if (a.after) r.after = a.rstd_after[there];
+  };
+  const auto put = [&](const Rows &to, int64_t i, const Eight &x) {
+    const int64_t there = i < a.rows ? i : a.rows - 1;
+    if (PIECES) Elem<T>::put8(to.base, there * to.stride + from, x);
+    else put_up_to8<T>(to.base, there * to.stride + from, n, x);
+  };
   int64_t i = (int64_t)blockIdx.x * kRows + which;
+  constexpr bool kAhead = sizeof(T) == 2;  // rows of 32 bits fill the registers as it is
+  Row next;
+  if (kAhead) ask(next, i);
   int turn = 0;
   for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.rows; first += stride, i += stride, turn ^= 1) {
-    const bool row = i < a.rows;
-    typename RowsOf<T>::Bits bits_d[HAS] = {}, bits_u[HAS] = {}, bits_y[HAS] = {}, bits_o[HAS] = {};
+    if (!kAhead) ask(next, i);
+    const Row now = next;
+    if (kAhead) ask(next, first + stride < a.rows ? i + stride : i);
+    const float before = a.before ? now.before : 0.f, after = a.after ? now.after : 1.f;
+    const float counts = kRows == 1 || i < a.rows ? 1.f : 0.f;
+    Eight d = RowsOf<T>::value(now.d, 8), k = RowsOf<T>::value(now.u, 8), y = RowsOf<T>::value(now.y, 8), h = RowsOf<T>::value(now.o, 8);
+    float sum[3] = {};
 #pragma unroll
-    for (int p = 0; p < HAS; ++p) {
-      const int64_t j = at + p * kApart;
-      const int has = row ? n[p] : 0;
-      if (a.dout.base) bits_d[p] = RowsOf<T>::ask(a.dout, i, j, has);
-      if (a.before) bits_y[p] = RowsOf<T>::ask(a.dy, i, j, has), bits_o[p] = RowsOf<T>::ask(a.out, i, j, has);
-      if (joins) bits_u[p] = RowsOf<T>::ask(a.u, i, j, has);
+    for (int c = 0; c < 8; ++c) {
+      d.v[c] = a.dout.base ? d.v[c] : 0.f;
+      y.v[c] = a.before ? y.v[c] : 0.f, h.v[c] = a.before ? h.v[c] * before : 0.f;
+      k.v[c] = joins ? k.v[c] * after : 0.f;
+      da.v[c] += y.v[c] * (kRows == 1 ? h.v[c] : h.v[c] * counts);
+      y.v[c] *= g.v[c];
+      d.v[c] += before * y.v[c];
+      const bool own = WHOLE || c >= others;
+      const float wk = own ? w.v[c] * k.v[c] : 0.f;
+      sum[0] += own ? y.v[c] * h.v[c] : 0.f, sum[1] += wk * d.v[c], sum[2] += wk * h.v[c];
     }
-    const float before = a.before && row ? a.rstd_before[i] : 0.f, after = a.after && row ? a.rstd_after[i] : 1.f;
-    Eight d[HAS];
-    float along = 0.f;
 #pragma unroll
-    for (int p = 0; p < HAS; ++p) {
-      d[p] = RowsOf<T>::value(bits_d[p], 8);
-      if (!a.before) continue;
-      const Eight dy = RowsOf<T>::value(bits_y[p], 8), o = RowsOf<T>::value(bits_o[p], 8);
+    for (int q = 0; q < 3; ++q) sum[q] = all_sum(sum[q]);
+    // (rows beyond the last are computed and stored as the last is: all have read it before one writes, as dx may be dout)
+    if (WAVES == 1) __syncthreads();
+    if (WAVES > 1) {
+      if ((threadIdx.x & 63) < 3) room[turn][threadIdx.x & 63][threadIdx.x >> 6] = (threadIdx.x & 63) == 0 ? sum[0] : (threadIdx.x & 63) == 1 ? sum[1] : sum[2];
+      __syncthreads();
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float h = o.v[k] * before;
-        da[p].v[k] += dy.v[k] * h;
-        along += dy.v[k] * g[p].v[k] * h;
+      for (int q = 0; q < 3; ++q) {
+        float x = room[turn][q][which * WAVES + threadIdx.x % WAVES];
+        x += moved<0xB1, 0xf>(x, 0.f);
+        if (WAVES >= 4) x += moved<0x4E, 0xf>(x, 0.f);
+        if (WAVES >= 8) x += moved<0x141, 0xf>(x, 0.f);
+        if (WAVES >= 16) x += moved<0x140, 0xf>(x, 0.f);
+        sum[q] = x;
       }
     }
-    if (a.before) {
-      along = row_sum<WAVES>(along, room[turn][0]) * each;
+    const float flow = before * (sum[0] * each), along = a.after ? (sum[1] - flow * sum[2]) * each : 0.f;
+    Eight du;
 #pragma unroll
-      for (int p = 0; p < HAS; ++p) {
-        const Eight dy = RowsOf<T>::value(bits_y[p], 8), o = RowsOf<T>::value(bits_o[p], 8);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) d[p].v[k] += before * (dy.v[k] * g[p].v[k] - o.v[k] * before * along);
-      }
+    for (int c = 0; c < 8; ++c) {
+      d.v[c] -= flow * h.v[c];
+      db.v[c] += d.v[c] * (kRows == 1 ? k.v[c] : k.v[c] * counts);
+      du.v[c] = after * (d.v[c] * w.v[c] - k.v[c] * along);
+      d.v[c] *= joins ? a.v.keep : 1.f;
     }
-    if (row && a.dx.base) {
-#pragma unroll
-      for (int p = 0; p < HAS; ++p) {
-        Eight dx;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) dx.v[k] = joins ? a.v.keep * d[p].v[k] : d[p].v[k];
-        put_up_to8<T>(a.dx.base, i * a.dx.stride + at + p * kApart, n[p], dx);
-      }
-    }
-    if (!joins) continue;
-    along = 0.f;
-#pragma unroll
-    for (int p = 0; p < HAS; ++p) {
-      const Eight u = RowsOf<T>::value(bits_u[p], 8);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float b = d[p].v[k] * (u.v[k] * after);
-        db[p].v[k] += b;
-        along += b * w[p].v[k];
-      }
-    }
-    along = a.after ? row_sum<WAVES>(along, room[turn][1]) * each : 0.f;
-    if (!row || !a.du.base) continue;
-#pragma unroll
-    for (int p = 0; p < HAS; ++p) {
-      Eight du = RowsOf<T>::value(bits_u[p], 8);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) du.v[k] = after * (d[p].v[k] * w[p].v[k] - du.v[k] * after * along);
-      put_up_to8<T>(a.du.base, i * a.du.stride + at + p * kApart, n[p], du);
+    if (BOTH || a.du.base) put(a.du, i, du);
+    if (BOTH || a.dx.base) put(a.dx, i, d);
+    if (kAhead) {
+      arrived(next.d), arrived(next.u), arrived(next.y), arrived(next.o);
+      asm volatile("" : "+v"(next.before), "+v"(next.after));
     }
   }
   if (!a.partial) return;
   const int64_t parts = gridDim.x;
-  if (kRows == 1) {
+  const auto put_line = [&](int s, const Eight &x) {
+    float *to = a.partial + (s * parts + blockIdx.x) * a.cols;
+    if (n >= 8) return put_up_to8<float>(to, at, 8, x);
 #pragma unroll
-    for (int p = 0; p < HAS; ++p) {
-      const int64_t j = at + p * kApart;
-      put_up_to8<float>(a.partial, blockIdx.x * a.cols + j, n[p], da[p]);
-      put_up_to8<float>(a.partial, (parts + blockIdx.x) * a.cols + j, n[p], db[p]);
-    }
+    for (int c = 0; c < 8; ++c)
+      if (c >= others && from + c < a.cols) to[from + c] = x.v[c];
+  };
+  if (kRows == 1) {
+    put_line(0, da), put_line(1, db);
     return;
   }
   // the rows' wavefronts are added in their order
@@ -295,9 +358,8 @@ __global__ __launch_bounds__(WIDE * 64) void ds_join_backward_kernel(JoinBackwar
   for (int s = 0; s < 2; ++s) {
     __syncthreads();
 #pragma unroll
-    for (int p = 0; p < HAS; ++p)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) lines[which][at + p * kApart + k] = s ? db[p].v[k] : da[p].v[k];
+    for (int c = 0; c < 8; ++c)
+      if (c >= others && from + c < a.cols) lines[which][from + c] = s ? db.v[c] : da.v[c];
     __syncthreads();
     for (int j = threadIdx.x; j < a.cols; j += WIDE * 64) {
       float sum = 0.f;
@@ -468,24 +530,24 @@ int64_t join_groups(int64_t rows, int64_t at_a_time, int64_t most) {
 template <typename T>
 int launch_forward(const JoinForward &a, hipStream_t stream) {
   const auto launch = [&](auto kernel, int rows, int waves) -> int {
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)join_groups(a.rows, rows, 256 * 32 / waves)), dim3(waves * 64), 0, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)join_groups(a.rows, rows, 256 * 16 / waves)), dim3(waves * 64), 0, stream, a);
     DS_HIP_TRY(hipGetLastError());
     return DS_OK;
   };
-  // few rows: as many wavefronts for each as have something to read
-  if (a.rows <= 256 && a.cols > 2048 && a.cols <= 8192) return launch(ds_join_forward_kernel<T, 16, 16, 1>, 1, 16);
-  if (a.cols <= 512) return launch(ds_join_forward_kernel<T, 1, 4, 1>, 4, 4);
-  if (a.cols <= 2048) return launch(ds_join_forward_kernel<T, 4, 4, 1>, 1, 4);
-  if (a.cols <= 4096) return launch(ds_join_forward_kernel<T, 4, 4, 2>, 1, 4);
-  if (a.cols <= 8192) return launch(ds_join_forward_kernel<T, 8, 8, 2>, 1, 8);
-  if (a.cols <= kLongest) return launch(ds_join_forward_kernel<T, 16, 16, 2, sizeof(T) == 2>, 1, 16);
+  if (a.cols < 8) return launch(ds_join_forward_kernel<T, 1, 8, 1, false>, 8, 8);
+  if (a.cols <= 512) return launch(ds_join_forward_kernel<T, 1, 8, 1, true>, 8, 8);
+  if (a.cols <= 1024) return launch(ds_join_forward_kernel<T, 2, 8, 1, true>, 4, 8);
+  if (a.cols <= 2048) return launch(ds_join_forward_kernel<T, 4, 8, 1, true>, 2, 8);
+  if (a.cols <= 4096) return launch(ds_join_forward_kernel<T, 8, 8, 1, true>, 1, 8);
+  if (a.cols <= 8192) return launch(ds_join_forward_kernel<T, 16, 16, 1, true>, 1, 16);
+  if (a.cols <= kLongest) return launch(ds_join_forward_kernel<T, 16, 16, 2, true>, 1, 16);
   return launch(ds_join_forward_long_kernel<T>, 1, 16);
 }
 
 int64_t join_parts(int64_t rows, int64_t cols) {
   if (rows <= 0) return 1;
-  if (cols <= 512) return join_groups(rows, 4, 512);
-  if (cols <= kLongestBackward) return join_groups(rows, 1, 512);
+  // work-groups of 16 wavefronts, one on each CU: as many lines as that takes
+  if (cols <= kLongestBackward) return join_groups(rows, cols <= 512 ? 16 : cols <= 1024 ? 8 : cols <= 2048 ? 4 : cols <= 4096 ? 2 : 1, 256);
   const int64_t across = (cols + 511) / 512;
   return join_groups(rows, 4, (1024 + across - 1) / across);
 }
@@ -499,10 +561,18 @@ int launch_backward(const JoinBackward &a, int64_t parts, hipStream_t stream) {
     DS_HIP_TRY(hipGetLastError());
     return DS_OK;
   };
-  if (a.cols <= 512) return launch(ds_join_backward_kernel<T, 1, 4, 1>, 4);
-  if (a.cols <= 2048) return launch(ds_join_backward_kernel<T, 4, 4, 1>, 4);
-  if (a.cols <= 4096) return launch(ds_join_backward_kernel<T, 8, 8, 1>, 8);
-  if (a.cols <= kLongestBackward) return launch(ds_join_backward_kernel<T, 16, 16, 1>, 16);
+  const auto of_width = [&](auto waves) -> int {
+    constexpr int kWaves = decltype(waves)::value;
+    if (!a.du.base || !a.dx.base) return launch(ds_join_backward_kernel<T, kWaves, 16, true, false, false>, 16);
+    if (kWaves > 1 && a.cols == kWaves * 512) return launch(ds_join_backward_kernel<T, kWaves, 16, true, kWaves != 1, true>, 16);
+    return launch(ds_join_backward_kernel<T, kWaves, 16, true, false, true>, 16);
+  };
+  if (a.cols < 8) return launch(ds_join_backward_kernel<T, 1, 16, false, false, false>, 16);
+  if (a.cols <= 512) return of_width(std::integral_constant<int, 1>());
+  if (a.cols <= 1024) return of_width(std::integral_constant<int, 2>());
+  if (a.cols <= 2048) return of_width(std::integral_constant<int, 4>());
+  if (a.cols <= 4096) return of_width(std::integral_constant<int, 8>());
+  if (a.cols <= kLongestBackward) return of_width(std::integral_constant<int, 16>());
   // the parameters' sums first: dx may be dout
   const dim3 grid((uint32_t)join_groups(a.rows, 1, 4096));
   float *alongs = nullptr;

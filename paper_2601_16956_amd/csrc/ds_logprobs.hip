@@ -152,23 +152,6 @@ __device__ inline void put_top(const Forward &a, int64_t i, int rank, uint64_t k
   if (a.top_logprobs) a.top_logprobs[i * a.top + rank] = bad ? __uint_as_float(0x7fc00000u) : key ? a.scale * (key_logit(key) - r.m) - logf(r.s) : -kInf;
 }
 
-// Over the wavefront, in every lane: neighbours, quads, eights, rows of 16, then rows' last lanes into the rows behind them.
-template <int CTRL, int ROWS>
-__device__ inline float moved(float x, float without) {
-  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(without), (int)__float_as_uint(x), CTRL, ROWS, 0xf, false));
-}
-__device__ inline float last_lane(float x) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63)); }
-__device__ inline float larger(float a, float b) { return a > b ? a : b; }
-__device__ inline float all_max(float x) {
-  x = larger(x, moved<0xB1, 0xf>(x, x)), x = larger(x, moved<0x4E, 0xf>(x, x)), x = larger(x, moved<0x141, 0xf>(x, x));
-  x = larger(x, moved<0x140, 0xf>(x, x)), x = larger(x, moved<0x142, 0xa>(x, x)), x = larger(x, moved<0x143, 0xc>(x, x));
-  return last_lane(x);
-}
-__device__ inline float all_sum(float x) {
-  x += moved<0xB1, 0xf>(x, 0.f), x += moved<0x4E, 0xf>(x, 0.f), x += moved<0x141, 0xf>(x, 0.f), x += moved<0x140, 0xf>(x, 0.f);
-  x += moved<0x142, 0xa>(x, 0.f), x += moved<0x143, 0xc>(x, 0.f);
-  return last_lane(x);
-}
 template <bool ENTROPY>
 __device__ inline Triple wave_triple(Triple a, float c) {
   raise<ENTROPY>(a, all_max(a.m), c);
@@ -453,7 +436,7 @@ __global__ __launch_bounds__(256) void ds_logprobs_backward_kernel(Backward a) {
 }
 
 // Bytes of a gradient from which on it is not to stay in the caches.
-constexpr int64_t kStream = 64 << 20;
+constexpr int64_t kStream = 256 << 20;
 
 // Parts of a row: where few rows leave most of the card idle, so many that the work-groups are about as many as the CUs, each of at least
 // kLeast columns, and no more candidates than the kernel that joins them has threads; but as many as it takes where the likeliest are looked for.

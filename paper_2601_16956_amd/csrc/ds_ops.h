@@ -510,6 +510,23 @@ __device__ inline float wave_sum(float x) {
   return x;
 }
 
+// The largest and the sum over the wavefront, in every lane, by moves between lanes (which do not go through LDS): neighbours, quads, eights, rows of 16, then rows' last lanes into the rows behind them.
+template <int CTRL, int ROWS>
+__device__ inline float moved(float x, float without) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(without), (int)__float_as_uint(x), CTRL, ROWS, 0xf, false));
+}
+__device__ inline float last_lane(float x) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63)); }
+__device__ inline float larger(float a, float b) { return a > b ? a : b; }
+__device__ inline float all_max(float x) {
+  x = larger(x, moved<0xB1, 0xf>(x, x)), x = larger(x, moved<0x4E, 0xf>(x, x)), x = larger(x, moved<0x141, 0xf>(x, x));
+  x = larger(x, moved<0x140, 0xf>(x, x)), x = larger(x, moved<0x142, 0xa>(x, x)), x = larger(x, moved<0x143, 0xc>(x, x));
+  return last_lane(x);
+}
+__device__ inline float all_sum(float x) {
+  x += moved<0xB1, 0xf>(x, 0.f), x += moved<0x4E, 0xf>(x, 0.f), x += moved<0x141, 0xf>(x, 0.f), x += moved<0x140, 0xf>(x, 0.f);
+  x += moved<0x142, 0xa>(x, 0.f), x += moved<0x143, 0xc>(x, 0.f);
+  return last_lane(x);
+}
 // out0[j] = partial[0][j] + partial[1][j] + ... over `parts` lines of `cols`, in an order that only their number decides; out1
 // likewise from the lines behind those.  Either may be NULL.
 int ds_launch_sum_parts(const float *partial, int64_t parts, int64_t cols, float *out0, float *out1, hipStream_t stream);

@@ -190,7 +190,7 @@ def test_join_backward(rows, cols, kind):
         assert all(m.rest_untouched() for m in (dout, dy, u, out, du, dx)) and da_rest() and dg_rest() and db_rest()
 
 
-@pytest.mark.parametrize("rows,cols", [(5, 300), (3, 4100), (3, 9000), (2, 20003)])
+@pytest.mark.parametrize("rows,cols", [(5, 300), (3, 4100), (3, 9000), (2, 20003), (4133, 301), (2051, 1001), (1029, 2009), (40, 7), (700, 4097)])
 def test_joins_in_place_are_the_same(rows, cols):
     rng = np.random.default_rng(cols)
     j = Joint(rng, cols, "bf16", True, True, True)
