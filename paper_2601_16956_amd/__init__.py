@@ -157,7 +157,7 @@ class ds_matmul_epilogue(ctypes.Structure):
 
 
 class ds_join(ctypes.Structure):
-    vectors = ()  # (what, elements) of the tensors that make_join took the vectors from
+    vectors = ()  # (what, elements, type) of the tensors that make_join took the vectors from
     _fields_ = [
         ("after_gamma", ctypes.c_void_p),
         ("gate", ctypes.c_void_p),
@@ -792,13 +792,14 @@ _byte_types: tuple = ()
 
 def _float_code(dtype) -> int:
     global _float_codes
+    code = _float_codes.get(dtype)
+    if code is not None:
+        return code
     if not _float_codes:
         import torch
         _float_codes = {torch.float32: DS_F32, torch.bfloat16: DS_BF16, torch.float16: DS_F16}
-    code = _float_codes.get(dtype)
-    if code is None:
-        raise TypeError(f"dtype {dtype} is none of float32, bfloat16 and float16")
-    return code
+        return _float_code(dtype)
+    raise TypeError(f"dtype {dtype} is none of float32, bfloat16 and float16")
 
 
 def make_matrix(tensor) -> ds_matrix:
@@ -849,12 +850,12 @@ def _vector(v, dtype: int, matrix: ds_matrix, axis: str, what: str):
     contiguous torch tensor on the GPU with an element of `dtype` for each of the matrix's rows or cols."""
     if v is None or not hasattr(v, "data_ptr"):
         return v
-    length = getattr(matrix, axis)
-    if _float_code(v.dtype) != dtype:
+    length = matrix.rows if axis == "rows" else matrix.cols
+    if _float_codes.get(v.dtype) != dtype and _float_code(v.dtype) != dtype:
         raise TypeError(f"{what} is {v.dtype}, not of the call's type")
     if not v.is_cuda:
         raise ValueError(f"{what} is not in device memory")
-    if v.dim() != 1 or v.shape[0] != length or (length > 1 and v.stride(0) != 1):
+    if v.shape != (length,) or not v.is_contiguous():
         raise ValueError(f"{what} is {length} elements next to each other, not {tuple(v.shape)} of strides {tuple(v.stride())}")
     return v.data_ptr()
 
@@ -950,26 +951,33 @@ def make_join(after: bool = False, after_gamma=None, gate=None, before: bool = F
     """Which norms a joint has, and its vectors: 1-D torch tensors on the GPU, contiguous, of one type, with an element for each column.
     (The structure keeps no tensor's memory.)"""
     made = ds_join(None, None, None, DS_F32, (DS_JOIN_AFTER if after else 0) | (DS_JOIN_BEFORE if before else 0), keep, scale, eps)
-    lengths, kind = [], None
-    for what, v in (("after_gamma", after_gamma), ("gate", gate), ("before_gamma", before_gamma)):
-        if v is None:
-            continue
-        if not v.is_cuda:
-            raise ValueError(f"{what} is not in device memory")
-        if v.dim() != 1 or (v.shape[0] > 1 and v.stride(0) != 1):
-            raise ValueError(f"{what} is one contiguous dimension")
-        code = _float_code(v.dtype)
-        if kind is not None and code != kind:
-            raise TypeError("the vectors of a joint are of one type")
-        made.param_dtype = kind = code
-        setattr(made, what, v.data_ptr())
-        lengths.append((what, v.shape[0]))
-    made.vectors = tuple(lengths)
+    vectors = []
+    if after_gamma is not None:
+        made.after_gamma = _joint_vector(after_gamma, "after_gamma", vectors)
+    if gate is not None:
+        made.gate = _joint_vector(gate, "gate", vectors)
+    if before_gamma is not None:
+        made.before_gamma = _joint_vector(before_gamma, "before_gamma", vectors)
+    if vectors:
+        made.param_dtype = vectors[0][2]
+        made.vectors = vectors
     return made
 
 
+def _joint_vector(v, what: str, vectors: list) -> int:
+    if not v.is_cuda:
+        raise ValueError(f"{what} is not in device memory")
+    shape, code = v.shape, _float_code(v.dtype)
+    if len(shape) != 1 or not v.is_contiguous():
+        raise ValueError(f"{what} is one contiguous dimension")
+    if vectors and vectors[0][2] != code:
+        raise TypeError("the vectors of a joint are of one type")
+    vectors.append((what, shape[0], code))
+    return v.data_ptr()
+
+
 def _fits(join: ds_join, cols: int) -> None:
-    for what, length in join.vectors:
+    for what, length, _ in join.vectors:
         if length != cols:
             raise ValueError(f"{what} has {length} elements for {cols} columns")
 

@@ -837,3 +837,27 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         assert same(written(), want)
     ds.ds_adamw_destroy(table)
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    """What the binding knows of a tensor and C does not of an address."""
+    f32 = lambda *shape: torch.zeros(*shape, device="cuda")  # noqa: E731
+    x, i64 = ds.make_matrix(f32(4, 40)), torch.zeros(4, dtype=torch.int64, device="cuda")
+    for call, kind in (
+            (lambda: ds.make_join(True, f32(40, 1)), ValueError), (lambda: ds.make_join(True, f32(80)[::2]), ValueError),
+            (lambda: ds.make_join(True, torch.zeros(40)), ValueError), (lambda: ds.make_join(True, f32(40), f32(40).half()), TypeError),
+            (lambda: ds.make_join(True, f32(40).double()), TypeError),
+            (lambda: ds.ds_join_forward(ds.make_join(True, f32(39)), x, x, x, None, None, None), ValueError),
+            (lambda: ds.ds_join_forward(ds.make_join(True, f32(40)), x, x, x, None, f32(5), None), ValueError),
+            (lambda: ds.ds_join_backward(ds.make_join(True, f32(40)), x, None, x, None, f32(4), None, x, x, f32(39)), ValueError),
+            (lambda: ds.ds_logprobs(x, 1.0, i64.int(), f32(4)), TypeError), (lambda: ds.ds_logprobs(x, 1.0, i64[:3], f32(4)), ValueError),
+            (lambda: ds.ds_logprobs(x, 1.0, i64.cpu(), f32(4)), ValueError), (lambda: ds.ds_logprobs(x, 1.0, i64, f32(3)), ValueError),
+            (lambda: ds.ds_logprobs(x, 1.0, i64, None, top=2, top_tokens=torch.zeros(4, 3, dtype=torch.int64, device="cuda")), ValueError),
+            (lambda: ds.ds_logprobs(x, 1.0, i64, None, top=2, top_logprobs=f32(4, 2).half()), TypeError),
+            (lambda: ds.ds_logprobs_backward(x, 1.0, i64, f32(4), f32(5), None, f32(4), None, x), ValueError),
+            (lambda: ds.make_adamw_settings(f32(1), 0.1), TypeError), (lambda: ds.make_adamw_settings(i64, 0.1), ValueError),
+            (lambda: ds.make_adamw_settings(i64[:1].cpu(), 0.1), ValueError), (lambda: ds.make_adamw_settings(i64[:1], 0.1, squares=f32(1)), TypeError),
+            (lambda: ds.make_uf8(torch.zeros(2, 32, dtype=torch.int8, device="cuda"), torch.zeros(2, 1, dtype=torch.uint8, device="cuda")), TypeError),
+            (lambda: ds.make_uf8(torch.zeros(2, 33, dtype=torch.uint8, device="cuda"), torch.zeros(2, 1, dtype=torch.uint8, device="cuda")), ValueError)):
+        with pytest.raises(kind):
+            call()
