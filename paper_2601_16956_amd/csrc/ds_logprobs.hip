@@ -185,6 +185,7 @@ __device__ inline Triple row_triple(Triple a, float c, Triple *room) {
 // How many of `count` keys are larger.  (Eight at a time are on their way; those behind the last are 0.)
 __device__ inline int rank_of(uint64_t key, const uint64_t *keys, int count) {
   int rank = 0;
+#pragma unroll 1
   for (int k = 0; k < count; k += 8)
 #pragma unroll
     for (int e = 0; e < 8; ++e) rank += keys[k + e] > key;
@@ -212,6 +213,7 @@ __device__ inline void likeliest(const T *row, int count, int64_t begin, uint32_
   int found;
   for (;;) {
     // pieces that have a column that reaches the bound, or (one of them) might have
+#pragma unroll 1
     for (int p = threadIdx.x; p < pieces; p += THREADS) {
       const float peak = peaks[p];
       if (peak > -kInf && key_of(peak, begin + p * W) >= bound) {
@@ -221,16 +223,14 @@ __device__ inline void likeliest(const T *row, int count, int64_t begin, uint32_
     }
     __syncthreads();
     const int hits = (int)room.n_hits;
-    for (int h = threadIdx.x; h < min(hits, kCandidates); h += THREADS) {
-      const int j = (int)room.hits[h] * W;
-      const Piece<T> x = piece_at(row, j, count);
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        const uint64_t key = key_of(x.v[k], begin + j + k);
-        if (x.v[k] > -kInf && key >= bound) {
-          const uint32_t at = atomicAdd(&room.count, 1u);
-          if (at < kCandidates) room.keys[at] = key;
-        }
+#pragma unroll 1
+    for (int e = threadIdx.x; e < min(hits, kCandidates) * W; e += THREADS) {
+      const int j = (int)room.hits[e / W] * W + e % W;
+      const float x = j < count ? Elem<T>::get(row, j) : -kInf;
+      const uint64_t key = key_of(x, begin + j);
+      if (x > -kInf && key >= bound) {
+        const uint32_t at = atomicAdd(&room.count, 1u);
+        if (at < kCandidates) room.keys[at] = key;
       }
     }
     __syncthreads();
@@ -238,6 +238,7 @@ __device__ inline void likeliest(const T *row, int count, int64_t begin, uint32_
     if (hits <= kCandidates && found <= kCandidates) break;
     __syncthreads();
     // a higher bound in every turn: at least kSample columns were found, no two keys are equal, and fewer are wanted
+#pragma unroll 1
     for (int at = threadIdx.x; at < kSample; at += THREADS)
       if (rank_of(room.keys[at], room.keys, kSample) == (int)top - 1) room.bound = room.keys[at];
     if (threadIdx.x == 0) room.n_hits = room.count = 0;
@@ -246,6 +247,7 @@ __device__ inline void likeliest(const T *row, int count, int64_t begin, uint32_
   }
   if (threadIdx.x < 8 && found + threadIdx.x < kCandidates) room.keys[found + threadIdx.x] = 0;
   __syncthreads();
+#pragma unroll 1
   for (int at = threadIdx.x; at < found; at += THREADS) {
     const uint64_t key = room.keys[at];
     const int rank = rank_of(key, room.keys, found);
@@ -359,7 +361,7 @@ __global__ __launch_bounds__(256) void ds_logprobs_join_kernel(Forward a) {
       __syncthreads();
       if (spare < 0) best[threadIdx.x] = 0;
       __syncthreads();
-      const int rank = key ? rank_of(key, keys, 256) : 256;
+      const int rank = key ? rank_of(key, keys, (int)(count - first < kMostKeys ? count - first : kMostKeys) + (int)DS_TOP_MOST) : 256;
       if (rank < (int)a.top) best[rank] = key;
     }
     __syncthreads();
