@@ -23,7 +23,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kEach = 2;                       // quads of a thread
 constexpr int64_t kQuads = kThreads * kEach;   // of a chunk
-constexpr int64_t kStream = 4 << 20;           // elements of a table from which on accesses are not temporal
+// Elements of a table from which on accesses are not temporal: its state is not to stay in the caches, and nothing else that does is to leave.
+// So / by ordinary accesses, us of the step, tables in rotation: float moments 1 M 6.8 / 8.2, 3 M 17.3 / 15.2, 6 M 31 / 29, 17 M 83 / 90, 55 M
+// 242 / 269; moments in 8 bits 6 M 24.2 / 23.8, 25 M 74 / 82, 136 M 362 / 390.
+constexpr int64_t kStream = 8 << 20;
 constexpr int64_t kSquareGroups = 2048;        // work-groups of the sum of squares, for each kind of tensors
 
 // A tensor in the table.  Its matrices are one row where that is how they lie; their strides are then not looked at.

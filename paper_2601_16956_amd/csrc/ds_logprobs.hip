@@ -437,17 +437,21 @@ __global__ __launch_bounds__(256) void ds_logprobs_backward_kernel(Backward a) {
   }
 }
 
-// Bytes of a gradient from which on it is not to stay in the caches.
-constexpr int64_t kStream = 256 << 20;
+// Bytes of a gradient from which on its accesses are not temporal: the gradient would leave the caches late, while others read.  So / by ordinary
+// accesses, us of the backward pass and the forward pass of the next rows: bf16, 32000 columns, 1024 rows (66 MB) 24 + 16 / 24 + 19, 2048 rows 47 +
+// 29 / 45 + 40, 4096 rows 92 + 54 / 89 + 73, 8192 rows 178 + 100 / 177 + 125.
+constexpr int64_t kStream = 64 << 20;
 
-// Parts of a row: where few rows leave most of the card idle, so many that the work-groups are about as many as the CUs, each of at least
-// kLeast columns, and no more candidates than the kernel that joins them has threads; but as many as it takes where the likeliest are looked for.
-constexpr int64_t kLeast = 32768;
+// Parts of a row: where few rows of more than kWhole columns leave most of the card idle, so many that the work-groups are about as many as the
+// CUs, each of at least kLeast columns, and no more candidates than the kernel that joins them has threads; but as many as it takes where the
+// likeliest are looked for.  bf16, us of both kernels, whole / in parts of 32768 columns / of 8192: 1 x 32000 with five likeliest 7.5 / - / 10.0,
+// 1 x 128000 - / 12.4 / 10.9 and without them 9.5 / 7.3 / 6.7, 16 x 128000 with five - / 14.1 / 12.6, 1 x 500000 without 28.8 / 7.8 / 6.8.
+constexpr int64_t kWhole = 32768, kLeast = 8192;
 int64_t part_cols_of(int64_t cols, int64_t parts) { return ((cols + parts - 1) / parts + 7) / 8 * 8; }
 int64_t parts_of(int64_t rows, int64_t cols, uint32_t top, int64_t size) {
   int64_t parts = 1;
-  if (rows <= 128) {
-    parts = std::min((256 + rows - 1) / rows, (cols + kLeast - 1) / kLeast);
+  if (rows <= 128 && cols > kWhole) {
+    parts = std::min(256 / rows, (cols + kLeast - 1) / kLeast);
     if (top) parts = std::min<int64_t>(parts, kMostKeys / top);
     parts = std::min<int64_t>(parts, 64);
   }
@@ -511,7 +515,10 @@ extern "C" int ds_logprobs(const ds_matrix *logits, float scale, const int64_t *
       };
       const auto rows_with = [&](auto likeliest) -> int {
         constexpr bool TOP = decltype(likeliest)::value;
-        if (cols <= 2048) return launch(ds_logprobs_kernel<T, 64, E, TOP>, 64, rows, pieces);
+        // One wavefront a row, four, or sixteen.  bf16, us: 4096 rows of 1024 columns 5.0 / 9.2 / -, of 4096 9.3 / 11.9 / -, of 8192 14.9 / 15.0 /
+        // -; 64 rows of 2048 3.3 / - / 4.0; 200 rows of 32000 - / 6.5 / 6.4, 300 rows - / 8.2 / 10.2, 512 rows with ten likeliest - / 17 / 22.
+        const int64_t bytes = cols * (int64_t)sizeof(T);
+        if (parts == 1 && bytes <= (rows > 256 ? 8192 : 4096)) return launch(ds_logprobs_kernel<T, 64, E, TOP>, 64, rows, pieces);
         if (rows * parts > 256) return launch(ds_logprobs_kernel<T, 256, E, TOP>, 256, rows * parts, pieces);
         return launch(ds_logprobs_kernel<T, 1024, E, TOP>, 1024, rows * parts, pieces);
       };
