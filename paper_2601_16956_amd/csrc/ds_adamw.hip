@@ -10,7 +10,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstring>
 #include <new>
 #include <type_traits>
 #include <utility>
@@ -28,6 +27,7 @@ constexpr int64_t kQuads = kThreads * kEach;   // of a chunk
 // 242 / 269; moments in 8 bits 6 M 24.2 / 23.8, 25 M 74 / 82, 136 M 362 / 390.
 constexpr int64_t kStream = 8 << 20;
 constexpr int64_t kSquareGroups = 2048;        // work-groups of the sum of squares, for each kind of tensors
+constexpr int kSquareChunks = 4;               // chunks that they have on their way at a time
 
 // A tensor in the table.  Its matrices are one row where that is how they lie; their strides are then not looked at.
 struct Tensor {
@@ -39,6 +39,15 @@ struct Tensor {
 struct Chunk {
   int64_t quad;  // the first one
   uint32_t tensor, reserved;
+};
+// A chunk of a tensor that is one row, with all that is needed of the tensor: one load away from the data.
+struct Flat {
+  void *param, *grad, *m, *v, *copy;  // of its first element
+  uint8_t *m_scale, *v_scale;
+  int32_t left;  // elements
+  uint32_t at;   // its first element's number
+  uint32_t number, copy_dtype;
+  float decay, rate;
 };
 // A kind of tensors: their types, whether they are one row, and their chunks.
 struct Kind {
@@ -186,14 +195,6 @@ __device__ inline void place_of(const Tensor &t, int64_t item, int64_t &i, int64
   const int64_t left = i < t.rows ? t.cols - j : 0;
   n = (int)(left < 0 ? 0 : left < 4 ? left : 4);
 }
-template <bool FLAT>
-__device__ inline void place(const Tensor &t, int64_t item, int64_t &i, int64_t &j, int &n) {
-  if (!FLAT) return place_of(t, item, i, j, n);
-  i = 0, j = item * 4;
-  const int64_t left = t.cols - j;
-  n = (int)(left < 0 ? 0 : left < 4 ? left : 4);
-}
-
 // The largest of eight neighbouring lanes', which hold a group of 32.
 __device__ inline uint32_t max_of_eight_lanes(uint32_t m) {
   m = max_of_four_lanes(m);
@@ -348,36 +349,29 @@ __device__ inline void step_chunk(const Tensor &t, int64_t quad, int left, const
   }
 }
 
-template <typename T>
-__device__ inline void advance(Rows &r, int64_t j) {
-  r.base = (T *)r.base + j;
-  if (r.scale) r.scale += j / kGroup;
+// A work-group takes a chunk, or several where a launch has no place for as many work-groups.  What it needs of the table is in scalar registers
+// before anything is written that the table might be.
+template <typename P, typename G, bool EIGHT, bool STREAM>
+__global__ __launch_bounds__(kThreads, 6) void ds_adamw_flat_kernel(const Flat *__restrict__ chunks, int64_t count, Settings s) {
+  __shared__ Now shared;
+  for (int64_t c = blockIdx.x; c < count; c += gridDim.x) {
+    const Flat f = chunks[c];
+    const auto row = [](void *base, uint8_t *scale) { return Rows{global(base), 0, global(scale), 0}; };
+    const Tensor t{row(f.param, nullptr), row(f.grad, nullptr), row(f.m, f.m_scale), row(f.v, f.v_scale), row(f.copy, nullptr), 1, f.left, 0,
+                   f.number, f.copy_dtype, f.decay, f.rate};
+    const bool begins = c == blockIdx.x;
+    if (f.left == kQuads * 4) step_chunk<P, G, EIGHT, true, STREAM, true>(t, f.at / 4, f.left, s, shared, begins);
+    else step_chunk<P, G, EIGHT, true, STREAM, false>(t, f.at / 4, f.left, s, shared, begins);
+  }
 }
-
-// A work-group takes a chunk, or several where a launch has no place for as many work-groups.
-template <typename P, typename G, bool EIGHT, bool FLAT, bool STREAM>
-__global__ __launch_bounds__(kThreads) void ds_adamw_step_kernel(const Tensor *__restrict__ tensors, const Chunk *__restrict__ chunks, int64_t count, Settings s) {
-  typedef std::conditional_t<EIGHT, uint8_t, float> M;
+template <typename P, typename G, bool EIGHT>
+__global__ __launch_bounds__(kThreads) void ds_adamw_rows_kernel(const Tensor *__restrict__ tensors, const Chunk *__restrict__ chunks, int64_t count, Settings s) {
   __shared__ Now shared;
   for (int64_t c = blockIdx.x; c < count; c += gridDim.x) {
     const Chunk chunk = chunks[c];
-    // whole, into scalar registers, before anything is written that it might be
     Tensor t = tensors[chunk.tensor];
     t.param = rows_of(t.param), t.grad = rows_of(t.grad), t.m = rows_of(t.m), t.v = rows_of(t.v), t.copy = rows_of(t.copy);
-    const bool begins = c == blockIdx.x;
-    if (!FLAT) {
-      step_chunk<P, G, EIGHT, FLAT, STREAM, false>(t, chunk.quad, 0, s, shared, begins);
-      continue;
-    }
-    const int64_t j = chunk.quad * 4, more = t.cols - j;
-    advance<P>(t.param, j), advance<G>(t.grad, j), advance<M>(t.m, j), advance<M>(t.v, j);
-    if (t.copy.base) {
-      if (t.copy_dtype == DS_F32) advance<float>(t.copy, j);
-      else advance<uint16_t>(t.copy, j);
-    }
-    const int left = (int)(more < kQuads * 4 ? more : kQuads * 4);
-    if (left == kQuads * 4) step_chunk<P, G, EIGHT, FLAT, STREAM, true>(t, chunk.quad, left, s, shared, begins);
-    else step_chunk<P, G, EIGHT, FLAT, STREAM, false>(t, chunk.quad, left, s, shared, begins);
+    step_chunk<P, G, EIGHT, false, false, false>(t, chunk.quad, 0, s, shared, c == blockIdx.x);
   }
 }
 
@@ -387,37 +381,63 @@ __device__ inline double wave_sum(double x) {
   return x;
 }
 
-// One sum for each work-group, in the order of its chunks; the next chunk's place is on its way while it adds.  (In 64 bits: gradients'
-// squares span more than 32 bits' exponents do, and the sums of ranks are added.)
-template <typename G, bool FLAT, bool STREAM>
-__global__ __launch_bounds__(kThreads) void ds_adamw_squares_kernel(const Tensor *__restrict__ tensors, const Chunk *__restrict__ chunks, int64_t count, double *partial) {
+// One sum for each work-group, in the order of its chunks.  (In 64 bits: gradients' squares span more than 32 bits' exponents do, and the
+// sums of ranks are added.)
+template <typename G>
+__device__ inline void add_squares(const typename QuadOf<G>::Bits &g, double &sum) {
+  const Four x = QuadOf<G>::value(g);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sum += (double)x.v[k] * (double)x.v[k];
+}
+__device__ inline void put_sum(double sum, double *partial) {
   __shared__ double sums[kThreads / 64];
-  double sum = 0.0;
-  Chunk chunk = chunks[blockIdx.x];
-  Tensor t = tensors[chunk.tensor];
-  for (int64_t c = blockIdx.x; c < count; c += gridDim.x) {
-    const Rows grad = rows_of(t.grad);
-    typename QuadOf<G>::Bits g[kEach];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      int64_t i, j;
-      int n;
-      place<FLAT>(t, chunk.quad + e * kThreads + threadIdx.x, i, j, n);
-      g[e] = ask_quad<G, STREAM>(grad.base, i * (FLAT ? 0 : grad.stride) + j, n);
-    }
-    chunk = chunks[c + gridDim.x < count ? c + gridDim.x : c];
-    t = tensors[chunk.tensor];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const Four x = QuadOf<G>::value(g[e]);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) sum += (double)x.v[k] * (double)x.v[k];
-    }
-  }
   sum = wave_sum(sum);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
   __syncthreads();
   if (threadIdx.x == 0) partial[blockIdx.x] = sums[0] + sums[1] + (sums[2] + sums[3]);
+}
+template <typename G, bool STREAM>
+__global__ __launch_bounds__(kThreads) void ds_adamw_squares_flat_kernel(const Flat *__restrict__ chunks, int64_t count, double *partial) {
+  double sum = 0.0;
+  for (int64_t c = (int64_t)blockIdx.x * kSquareChunks; c < count; c += (int64_t)gridDim.x * kSquareChunks) {
+    const void *from[kSquareChunks];
+    int left[kSquareChunks];
+#pragma unroll
+    for (int u = 0; u < kSquareChunks; ++u) {
+      const Flat &f = chunks[c + u < count ? c + u : c];
+      from[u] = global((const void *)f.grad), left[u] = c + u < count ? f.left : 0;
+    }
+    typename QuadOf<G>::Bits g[kSquareChunks][kEach];
+#pragma unroll
+    for (int u = 0; u < kSquareChunks; ++u)
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int j = (e * kThreads + threadIdx.x) * 4, more = left[u] - j;
+        g[u][e] = ask_quad<G, STREAM>(from[u], j, more < 0 ? 0 : more < 4 ? more : 4);
+      }
+#pragma unroll
+    for (int u = 0; u < kSquareChunks; ++u)
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) add_squares<G>(g[u][e], sum);
+  }
+  put_sum(sum, partial);
+}
+template <typename G>
+__global__ __launch_bounds__(kThreads) void ds_adamw_squares_rows_kernel(const Tensor *__restrict__ tensors, const Chunk *__restrict__ chunks, int64_t count, double *partial) {
+  double sum = 0.0;
+  for (int64_t c = blockIdx.x; c < count; c += gridDim.x) {
+    const Chunk chunk = chunks[c];
+    const Tensor &t = tensors[chunk.tensor];
+    const Rows grad = rows_of(t.grad);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      int64_t i, j;
+      int n;
+      place_of(t, chunk.quad + e * kThreads + threadIdx.x, i, j, n);
+      add_squares<G>(ask_quad<G, false>(grad.base, i * grad.stride + j, n), sum);
+    }
+  }
+  put_sum(sum, partial);
 }
 
 __global__ __launch_bounds__(1024) void ds_adamw_squares_sum_kernel(const double *partial, int64_t count, double *squares) {
@@ -433,7 +453,10 @@ __global__ __launch_bounds__(1024) void ds_adamw_squares_sum_kernel(const double
   *squares = sum;
 }
 
-int64_t square_groups(const Kind &k) { return std::min(k.end - k.begin, kSquareGroups); }
+int64_t square_groups(const Kind &k) {
+  const int64_t chunks = k.end - k.begin;
+  return std::min(k.flat ? (chunks + kSquareChunks - 1) / kSquareChunks : chunks, kSquareGroups);
+}
 
 // Memory that a step writes.
 struct Range {
@@ -465,8 +488,9 @@ bool written_twice(std::vector<Range> &ranges) {
 struct ds_adamw {
   int device = -1;
   void *memory = nullptr;
-  const Tensor *tensors = nullptr;
-  const Chunk *chunks = nullptr;
+  const Tensor *tensors = nullptr;  // those of rows
+  const Chunk *chunks = nullptr;    // theirs
+  const Flat *flats = nullptr;      // those of tensors that are one row
   std::vector<Kind> kinds;
   int64_t elements = 0;
   int64_t parts() const {
@@ -535,28 +559,44 @@ int make_table(const ds_adamw_tensor *from, size_t n, ds_adamw &table) {
   }
   if (written_twice(written)) return DS_EOVERLAP;
   std::stable_sort(order.begin(), order.end(), [](const auto &a, const auto &b) { return a.first < b.first; });
+  std::vector<Tensor> of_rows;
   std::vector<Chunk> chunks;
+  std::vector<Flat> flats;
   for (size_t k = 0; k < order.size(); ++k) {
-    const uint32_t kind = order[k].first, at = order[k].second;
-    if (k == 0 || order[k - 1].first != kind) table.kinds.push_back({kind / 12, kind / 4 % 3, kind / 2 % 2, kind % 2, (int64_t)chunks.size(), 0});
-    const int64_t all = tensors[at].rows * tensors[at].quads;
-    for (int64_t quad = 0; quad < all; quad += kQuads) chunks.push_back({quad, at, 0});
-    table.kinds.back().end = (int64_t)chunks.size();
+    const uint32_t kind = order[k].first;
+    const Tensor &t = tensors[order[k].second];
+    const bool flat = kind % 2;
+    if (k == 0 || order[k - 1].first != kind)
+      table.kinds.push_back({kind / 12, kind / 4 % 3, kind / 2 % 2, kind % 2, (int64_t)(flat ? flats.size() : chunks.size()), 0});
+    if (flat) {
+      const Kind &of = table.kinds.back();
+      const int64_t m = of.eight ? 1 : 4, copy = ds_itemsize(t.copy_dtype);
+      const auto at = [](const void *base, int64_t bytes) { return base ? (void *)((uint8_t *)base + bytes) : nullptr; };
+      for (int64_t j = 0; j < t.cols; j += kQuads * 4)
+        flats.push_back({at(t.param.base, j * ds_itemsize(of.param)), at(t.grad.base, j * ds_itemsize(of.grad)), at(t.m.base, j * m), at(t.v.base, j * m),
+                         at(t.copy.base, j * copy), (uint8_t *)at(t.m.scale, j / kGroup), (uint8_t *)at(t.v.scale, j / kGroup),
+                         (int32_t)std::min(t.cols - j, kQuads * 4), (uint32_t)j, t.number, t.copy_dtype, t.decay, t.rate});
+    } else {
+      for (int64_t quad = 0; quad < t.rows * t.quads; quad += kQuads) chunks.push_back({quad, (uint32_t)of_rows.size(), 0});
+      of_rows.push_back(t);
+    }
+    table.kinds.back().end = (int64_t)(flat ? flats.size() : chunks.size());
   }
   DS_HIP_TRY(hipGetDevice(&table.device));
   if (tensors.empty()) return DS_OK;
-  const size_t first = tensors.size() * sizeof(Tensor), second = chunks.size() * sizeof(Chunk);
-  std::vector<uint8_t> all(first + second);
-  std::memcpy(all.data(), tensors.data(), first);
-  std::memcpy(all.data() + first, chunks.data(), second);
+  const size_t sizes[] = {of_rows.size() * sizeof(Tensor), chunks.size() * sizeof(Chunk), flats.size() * sizeof(Flat)};
+  std::vector<uint8_t> all(sizes[0] + sizes[1] + sizes[2]);
+  std::copy_n((const uint8_t *)of_rows.data(), sizes[0], all.data());
+  std::copy_n((const uint8_t *)chunks.data(), sizes[1], all.data() + sizes[0]);
+  std::copy_n((const uint8_t *)flats.data(), sizes[2], all.data() + sizes[0] + sizes[1]);
   const hipError_t e = hipMalloc(&table.memory, all.size());
   if (e == hipErrorOutOfMemory) {
     (void)hipGetLastError();
     return DS_ENOMEM;
   }
   DS_HIP_TRY(e);
-  table.tensors = (const Tensor *)table.memory;
-  table.chunks = (const Chunk *)((const uint8_t *)table.memory + first);
+  const uint8_t *at = (const uint8_t *)table.memory;
+  table.tensors = (const Tensor *)at, table.chunks = (const Chunk *)(at + sizes[0]), table.flats = (const Flat *)(at + sizes[0] + sizes[1]);
   DS_HIP_TRY(hipMemcpy(table.memory, all.data(), all.size(), hipMemcpyHostToDevice));
   return DS_OK;
 }
@@ -617,14 +657,14 @@ extern "C" int ds_adamw_squares(const ds_adamw *table, double *squares, void *wo
     const int64_t groups = square_groups(k);
     DS_TRY(ds_with_type(k.grad, [&](auto type) -> int {
       typedef decltype(type) G;
-      const auto launch = [&](auto kernel) -> int {
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(kThreads), 0, (hipStream_t)stream, table->tensors, table->chunks + k.begin,
-                           k.end - k.begin, partial);
+      const auto launch = [&](auto kernel, auto... table_of) -> int {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(kThreads), 0, (hipStream_t)stream, table_of..., k.end - k.begin, partial);
         DS_HIP_TRY(hipGetLastError());
         return DS_OK;
       };
-      if (!k.flat) return launch(ds_adamw_squares_kernel<G, false, false>);
-      return table->elements < kStream ? launch(ds_adamw_squares_kernel<G, true, false>) : launch(ds_adamw_squares_kernel<G, true, true>);
+      if (!k.flat) return launch(ds_adamw_squares_rows_kernel<G>, table->tensors, table->chunks + k.begin);
+      return table->elements < kStream ? launch(ds_adamw_squares_flat_kernel<G, false>, table->flats + k.begin)
+                                       : launch(ds_adamw_squares_flat_kernel<G, true>, table->flats + k.begin);
     }));
     partial += groups;
   }
@@ -650,17 +690,18 @@ extern "C" int ds_adamw_step(const ds_adamw *table, const ds_adamw_settings *set
       typedef decltype(type) P;
       return ds_with_type(k.grad, [&](auto grad) -> int {
         typedef decltype(grad) G;
-        const auto launch = [&](auto kernel) -> int {
-          hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(count, kMaxGrid)), dim3(kThreads), 0, (hipStream_t)stream, table->tensors,
-                             table->chunks + k.begin, count, s);
+        const auto launch = [&](auto kernel, auto... table_of) -> int {
+          hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(count, kMaxGrid)), dim3(kThreads), 0, (hipStream_t)stream, table_of..., count, s);
           DS_HIP_TRY(hipGetLastError());
           return DS_OK;
         };
         if (!k.flat)
-          return k.eight ? launch(ds_adamw_step_kernel<P, G, true, false, false>) : launch(ds_adamw_step_kernel<P, G, false, false, false>);
+          return k.eight ? launch(ds_adamw_rows_kernel<P, G, true>, table->tensors, table->chunks + k.begin)
+                         : launch(ds_adamw_rows_kernel<P, G, false>, table->tensors, table->chunks + k.begin);
+        const Flat *flats = table->flats + k.begin;
         if (table->elements < kStream)
-          return k.eight ? launch(ds_adamw_step_kernel<P, G, true, true, false>) : launch(ds_adamw_step_kernel<P, G, false, true, false>);
-        return k.eight ? launch(ds_adamw_step_kernel<P, G, true, true, true>) : launch(ds_adamw_step_kernel<P, G, false, true, true>);
+          return k.eight ? launch(ds_adamw_flat_kernel<P, G, true, false>, flats) : launch(ds_adamw_flat_kernel<P, G, false, false>, flats);
+        return k.eight ? launch(ds_adamw_flat_kernel<P, G, true, true>, flats) : launch(ds_adamw_flat_kernel<P, G, false, true>, flats);
       });
     }));
   }
