@@ -855,7 +855,7 @@ def _vector(v, dtype: int, matrix: ds_matrix, axis: str, what: str):
         raise TypeError(f"{what} is {v.dtype}, not of the call's type")
     if not v.is_cuda:
         raise ValueError(f"{what} is not in device memory")
-    if v.shape != (length,) or not v.is_contiguous():
+    if v.dim() != 1 or v.shape[0] != length or (length > 1 and v.stride(0) != 1):
         raise ValueError(f"{what} is {length} elements next to each other, not {tuple(v.shape)} of strides {tuple(v.stride())}")
     return v.data_ptr()
 
