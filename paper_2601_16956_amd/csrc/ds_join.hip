@@ -57,6 +57,28 @@ __device__ inline void arrived(B &bits) {
     for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(bits.w[q][k]));
 }
 
+// Eight elements of a row; STREAM: not temporal, where a wavefront's are 1 KiB without a gap.
+template <typename T, bool STREAM>
+__device__ inline typename RowsOf<T>::Bits ask_eight(const Rows &m, int64_t i, int64_t j) {
+  if constexpr (STREAM && sizeof(T) == 2) {
+    typename RowsOf<T>::Bits b;
+    b.w[0] = __builtin_nontemporal_load((const ds_u32x4 *)((const T *)m.base + i * m.stride + j));
+    return b;
+  } else {
+    return RowsOf<T>::ask(m, i, j, 8);
+  }
+}
+template <typename T, bool STREAM>
+__device__ inline void put_eight(const Rows &m, int64_t i, int64_t j, const Eight &x) {
+  if constexpr (STREAM && sizeof(T) == 2) {
+    ds_u32x4 bits;
+    Elem<T>::put8(&bits, 0, x);
+    __builtin_nontemporal_store(bits, (ds_u32x4 *)((T *)m.base + i * m.stride + j));
+  } else {
+    Elem<T>::put8(m.base, i * m.stride + j, x);
+  }
+}
+
 // What eight elements of out are when they are read back.
 template <typename T>
 __device__ inline void as_stored(Eight &e) {
@@ -94,7 +116,7 @@ __device__ inline float total_of_row(float x, float *room, int which) {
 // the last row's stores too, elsewhere.  So, from a row of a piece on (PIECES), every load and store is made: a piece that is not whole is the row's
 // last eight columns, left out of the sums where others have them, but computed and stored as they do; rows beyond the last are the last;
 // without a block x is read for u.  Nothing is stored before the whole row has been read: out may be x.
-template <typename T, int WAVES, int WIDE, int HAS, bool PIECES>
+template <typename T, int WAVES, int WIDE, int HAS, bool PIECES, bool STREAM>
 __global__ __launch_bounds__(WIDE * 64) void ds_join_forward_kernel(JoinForward a) {
   __shared__ float room[2][2][WIDE];
   constexpr int kRows = WIDE / WAVES, kApart = WAVES * 512;
@@ -118,12 +140,14 @@ __global__ __launch_bounds__(WIDE * 64) void ds_join_forward_kernel(JoinForward 
   const auto ask = [&](int64_t i) {
     const int64_t there = i < a.rows ? i : a.rows - 1;
 #pragma unroll
-    for (int p = 0; p < HAS; ++p)
-      next_x[p] = RowsOf<T>::ask(a.x, there, from[p], PIECES ? 8 : n[p]), next_u[p] = RowsOf<T>::ask(u_or_x, there, from[p], PIECES ? 8 : n[p]);
+    for (int p = 0; p < HAS; ++p) {
+      next_x[p] = PIECES ? ask_eight<T, STREAM>(a.x, there, from[p]) : RowsOf<T>::ask(a.x, there, from[p], n[p]);
+      next_u[p] = PIECES ? ask_eight<T, STREAM>(u_or_x, there, from[p]) : RowsOf<T>::ask(u_or_x, there, from[p], n[p]);
+    }
   };
   const auto put = [&](const Rows &to, int64_t i, int p, const Eight &x) {
     const int64_t there = i < a.rows ? i : a.rows - 1;
-    if (PIECES) Elem<T>::put8(to.base, there * to.stride + from[p], x);
+    if (PIECES) put_eight<T, STREAM>(to, there, from[p], x);
     else put_up_to8<T>(to.base, there * to.stride + from[p], n[p], x);
   };
   constexpr bool kAhead = sizeof(T) == 2 || HAS == 1;  // where the registers hold both rows
@@ -238,7 +262,7 @@ struct JoinBackward {
 // a row of a piece on (PIECES), every load and store is made: a piece that is not whole is the row's last eight columns, left out of the
 // sums where others have them, but computed and stored as they do; rows beyond the last are the last; what there is none of is read from
 // where there is something.  WHOLE: all pieces are whole and the threads' own.  BOTH: du and dx are wanted.
-template <typename T, int WAVES, int WIDE, bool PIECES, bool WHOLE, bool BOTH>
+template <typename T, int WAVES, int WIDE, bool PIECES, bool WHOLE, bool BOTH, bool STREAM>
 __global__ __launch_bounds__(WIDE * 64) void ds_join_backward_kernel(JoinBackward a) {
   constexpr int kRows = WIDE / WAVES, kApart = WAVES * 512;
   __shared__ float room[2][3][WIDE];
@@ -266,8 +290,8 @@ __global__ __launch_bounds__(WIDE * 64) void ds_join_backward_kernel(JoinBackwar
   const auto ask = [&](Row &r, int64_t i) {
     const int64_t there = i < a.rows ? i : a.rows - 1;
     if (PIECES) {
-      r.d = RowsOf<T>::ask(s.dout, there, from, 8), r.u = RowsOf<T>::ask(s.u, there, from, 8);
-      r.y = RowsOf<T>::ask(s.dy, there, from, 8), r.o = RowsOf<T>::ask(s.out, there, from, 8);
+      r.d = ask_eight<T, STREAM>(s.dout, there, from), r.u = ask_eight<T, STREAM>(s.u, there, from);
+      r.y = ask_eight<T, STREAM>(s.dy, there, from), r.o = ask_eight<T, STREAM>(s.out, there, from);
       r.before = s.rstd_before[there], r.after = s.rstd_after[there];
       return;
     }
@@ -279,7 +303,7 @@ __global__ __launch_bounds__(WIDE * 64) void ds_join_backward_kernel(JoinBackwar
   };
   const auto put = [&](const Rows &to, int64_t i, const Eight &x) {
     const int64_t there = i < a.rows ? i : a.rows - 1;
-    if (PIECES) Elem<T>::put8(to.base, there * to.stride + from, x);
+    if (PIECES) put_eight<T, STREAM>(to, there, from, x);
     else put_up_to8<T>(to.base, there * to.stride + from, n, x);
   };
   int64_t i = (int64_t)blockIdx.x * kRows + which;
@@ -527,6 +551,15 @@ int64_t join_groups(int64_t rows, int64_t at_a_time, int64_t most) {
   return sets < most ? sets : most;
 }
 
+// Bytes that a call moves from which on its accesses are not temporal: no cache holds them until someone else reads them.  So / by ordinary
+// accesses, us, bf16, rows of 4096: forward 8192 rows (268 MB) 47.4 / 52.9, 2048 rows (67 MB) 15.6 / 14.5; backward with the lines' sums 8192 rows (403 MB)
+// 77.1 / 85.5, 2048 rows (101 MB) 30.6 / 29.8.
+constexpr int64_t kStream = 256 << 20;
+template <typename T>
+bool streams(int64_t elements) {
+  return sizeof(T) == 2 && elements >= kStream / 2;
+}
+
 template <typename T>
 int launch_forward(const JoinForward &a, hipStream_t stream) {
   const auto launch = [&](auto kernel, int rows, int waves) -> int {
@@ -534,13 +567,17 @@ int launch_forward(const JoinForward &a, hipStream_t stream) {
     DS_HIP_TRY(hipGetLastError());
     return DS_OK;
   };
-  if (a.cols < 8) return launch(ds_join_forward_kernel<T, 1, 8, 1, false>, 8, 8);
-  if (a.cols <= 512) return launch(ds_join_forward_kernel<T, 1, 8, 1, true>, 8, 8);
-  if (a.cols <= 1024) return launch(ds_join_forward_kernel<T, 2, 8, 1, true>, 4, 8);
-  if (a.cols <= 2048) return launch(ds_join_forward_kernel<T, 4, 8, 1, true>, 2, 8);
-  if (a.cols <= 4096) return launch(ds_join_forward_kernel<T, 8, 8, 1, true>, 1, 8);
-  if (a.cols <= 8192) return launch(ds_join_forward_kernel<T, 16, 16, 1, true>, 1, 16);
-  if (a.cols <= kLongest) return launch(ds_join_forward_kernel<T, 16, 16, 2, true>, 1, 16);
+  if (a.cols < 8) return launch(ds_join_forward_kernel<T, 1, 8, 1, false, false>, 8, 8);
+  const auto of_width = [&](auto streams) -> int {
+    constexpr bool STREAM = decltype(streams)::value;
+    if (a.cols <= 512) return launch(ds_join_forward_kernel<T, 1, 8, 1, true, STREAM>, 8, 8);
+    if (a.cols <= 1024) return launch(ds_join_forward_kernel<T, 2, 8, 1, true, STREAM>, 4, 8);
+    if (a.cols <= 2048) return launch(ds_join_forward_kernel<T, 4, 8, 1, true, STREAM>, 2, 8);
+    if (a.cols <= 4096) return launch(ds_join_forward_kernel<T, 8, 8, 1, true, STREAM>, 1, 8);
+    if (a.cols <= 8192) return launch(ds_join_forward_kernel<T, 16, 16, 1, true, STREAM>, 1, 16);
+    return launch(ds_join_forward_kernel<T, 16, 16, 2, true, STREAM>, 1, 16);
+  };
+  if (a.cols <= kLongest) return streams<T>(4 * a.rows * a.cols) ? of_width(std::integral_constant<bool, sizeof(T) == 2>()) : of_width(std::false_type());
   return launch(ds_join_forward_long_kernel<T>, 1, 16);
 }
 
@@ -563,11 +600,16 @@ int launch_backward(const JoinBackward &a, int64_t parts, hipStream_t stream) {
   };
   const auto of_width = [&](auto waves) -> int {
     constexpr int kWaves = decltype(waves)::value;
-    if (!a.du.base || !a.dx.base) return launch(ds_join_backward_kernel<T, kWaves, 16, true, false, false>, 16);
-    if (kWaves > 1 && a.cols == kWaves * 512) return launch(ds_join_backward_kernel<T, kWaves, 16, true, kWaves != 1, true>, 16);
-    return launch(ds_join_backward_kernel<T, kWaves, 16, true, false, true>, 16);
+    constexpr bool S = sizeof(T) == 2;
+    const bool whole = kWaves > 1 && a.cols == kWaves * 512;
+    if (!a.du.base || !a.dx.base) return launch(ds_join_backward_kernel<T, kWaves, 16, true, false, false, false>, 16);
+    if (streams<T>(6 * a.rows * a.cols))
+      return whole ? launch(ds_join_backward_kernel<T, kWaves, 16, true, kWaves != 1, true, S>, 16)
+                   : launch(ds_join_backward_kernel<T, kWaves, 16, true, false, true, S>, 16);
+    return whole ? launch(ds_join_backward_kernel<T, kWaves, 16, true, kWaves != 1, true, false>, 16)
+                 : launch(ds_join_backward_kernel<T, kWaves, 16, true, false, true, false>, 16);
   };
-  if (a.cols < 8) return launch(ds_join_backward_kernel<T, 1, 16, false, false, false>, 16);
+  if (a.cols < 8) return launch(ds_join_backward_kernel<T, 1, 16, false, false, false, false>, 16);
   if (a.cols <= 512) return of_width(std::integral_constant<int, 1>());
   if (a.cols <= 1024) return of_width(std::integral_constant<int, 2>());
   if (a.cols <= 2048) return of_width(std::integral_constant<int, 4>());

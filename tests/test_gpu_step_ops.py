@@ -861,3 +861,102 @@ def test_tensors_that_do_not_fit_are_refused():
             (lambda: ds.make_uf8(torch.zeros(2, 33, dtype=torch.uint8, device="cuda"), torch.zeros(2, 1, dtype=torch.uint8, device="cuda")), ValueError)):
         with pytest.raises(kind):
             call()
+
+
+# ---- large calls, whose accesses are others, against calls on their parts ---------------------------------------
+
+@pytest.mark.parametrize("rows,cols,shift", [(9000, 4096, 0), (21000, 2040, 1), (40100, 1001, 0), (2900, 12000, 3)])
+def test_large_joins_are_their_rows(rows, cols, shift):
+    torch.manual_seed(rows)
+    wide = lambda: torch.randn(rows * cols + shift + 8, device="cuda").bfloat16()[shift:shift + rows * cols].view(rows, cols)  # noqa: E731
+    u, x, dout, dy = wide(), wide(), wide(), wide()
+    vectors = [torch.randn(cols, device="cuda").bfloat16() for _ in range(3)]
+    j = ds.make_join(True, vectors[0], vectors[1], True, vectors[2], 0.5, 2.0, 1e-5)
+    M, parts = ds.make_matrix, [slice(k, min(k + 3000, rows)) for k in range(0, rows, 3000)]
+
+    def run(pieces):
+        out, y, du, dx = (torch.empty_like(u) for _ in range(4))
+        ra, rb = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        sums = []
+        for k in pieces:
+            n = u[k].shape[0]
+            ds.ds_join_forward(j, M(u[k]), M(x[k]), M(out[k]), M(y[k]), ra[k], rb[k], stream())
+            need = ds.ds_join_backward_workspace(n, cols)
+            ws, rest = workspace(need)
+            three = [torch.empty(cols, device="cuda") for _ in range(3)]
+            ds.ds_join_backward(j, M(dout[k]), M(dy[k]), M(u[k]), M(out[k]), ra[k], rb[k], M(du[k]), M(dx[k]), *three, ws.data_ptr(), need, stream())
+            assert rest()
+            sums.append(torch.stack(three).double())
+        return [out, y, du, dx, ra, rb], sum(sums)
+    (whole, sums), (pieced, added) = run([slice(0, rows)]), run(parts)
+    assert same(whole, pieced)
+    # the same terms in another order: chains of less than 2^9 sums, and those of a work-group's rows, of terms that are random
+    assert ((sums - added).norm(dim=1) <= 2.0 ** -24 * 512 * sums.norm(dim=1)).all()
+
+
+def test_large_gradients_of_log_probabilities_are_their_rows():
+    rows, cols = 1200, 32011
+    torch.manual_seed(3)
+    z, tokens = (torch.randn(rows, cols, device="cuda") * 3).bfloat16(), torch.randint(0, cols, (rows,), device="cuda")
+    up, along = torch.randn(rows, device="cuda"), torch.randn(rows, device="cuda")
+    M, stats = ds.make_matrix, [torch.empty(rows, device="cuda") for _ in range(4)]
+    ds.ds_logprobs(M(z), 0.9, tokens, *stats, stream=stream())
+    for b in (None, along):
+        whole, pieced = torch.empty_like(z), torch.empty_like(z)
+        ds.ds_logprobs_backward(M(z), 0.9, tokens, *stats[1:], up, b, M(whole), stream())
+        for k in range(0, rows, 300):
+            k = slice(k, k + 300)
+            ds.ds_logprobs_backward(M(z[k]), 0.9, tokens[k], *[s[k] for s in stats[1:]], up[k], b[k] if b is not None else None, M(pieced[k]), stream())
+        assert torch.equal(whole, pieced)
+        ds.ds_logprobs_backward(M(z.clone()), 0.9, tokens, *stats[1:], up, b, M(pieced), stream())
+        assert torch.equal(whole, pieced)
+    at = z.clone()
+    ds.ds_logprobs_backward(M(at), 0.9, tokens, *stats[1:], up, along, M(at), stream())
+    assert torch.equal(at, whole)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_a_large_update_is_its_tensors(eight):
+    n = (4 << 20) + 37
+    nothing = ds.make_adamw_tensor(*[ds.ds_matrix(None, ds.DS_F32, 0, 0, 5, 5, 1, None, 0)] * 4)
+
+    def make():
+        torch.manual_seed(5)
+        entries, tensors = [], []
+        for _ in range(3):
+            param, grad = torch.randn(1, n, device="cuda"), torch.randn(1, n, device="cuda").bfloat16()
+            copy = torch.zeros(1, n, dtype=torch.bfloat16, device="cuda")
+            if eight:
+                qm, qv = torch.randint(-127, 128, (1, n), dtype=torch.int8, device="cuda"), torch.randint(0, 256, (1, n), dtype=torch.uint8, device="cuda")
+                sm, sv = (torch.randint(100, 110, (1, -(-n // 32)), dtype=torch.uint8, device="cuda") for _ in range(2))
+                state, m, v = [qm, sm, qv, sv], ds.make_mx8(qm, sm), ds.make_uf8(qv, sv)
+            else:
+                state = [torch.randn(1, n, device="cuda"), torch.rand(1, n, device="cuda")]
+                m, v = (ds.make_matrix(t) for t in state)
+            entries.append(ds.make_adamw_tensor(ds.make_matrix(param), ds.make_matrix(grad), m, v, ds.make_matrix(copy), 0.1))
+            tensors += [param, copy, *state, grad]
+        return entries, tensors
+    step, squares = torch.full((1,), 9, dtype=torch.int64, device="cuda"), torch.zeros(2, dtype=torch.float64, device="cuda")
+    s = ds.make_adamw_settings(step, 1e-2, seed=12)
+
+    def squares_of(table, to):
+        need = ds.ds_adamw_squares_workspace(table)
+        ws, rest = workspace(need)
+        ds.ds_adamw_squares(table, to, ws.data_ptr(), need, stream())
+        assert rest()
+    entries, whole = make()
+    table = ds.ds_adamw_create(entries)
+    squares_of(table, squares[:1])
+    ds.ds_adamw_step(table, s, stream())
+    torch.cuda.synchronize()
+    ds.ds_adamw_destroy(table)
+    entries, pieced = make()
+    total = 0.0
+    for k in range(3):
+        table = ds.ds_adamw_create([nothing] * k + [entries[k]])
+        squares_of(table, squares[1:])
+        ds.ds_adamw_step(table, s, stream())
+        torch.cuda.synchronize()
+        total += float(squares[1])
+        ds.ds_adamw_destroy(table)
+    assert same(whole, pieced) and abs(float(squares[0]) - total) <= 1e-12 * total
