@@ -825,7 +825,7 @@ int ds_join_backward(const ds_join *join, const ds_matrix *dout, const ds_matrix
 
 /*
  * Log probabilities of given tokens.  With z = scale * x over a row of the logits
- * x (DS_F32, DS_BF16, DS_F16; ROWS), scale > 0 and finite (1 / temperature):
+ * x (DS_F32, DS_BF16, DS_F16; ROWS), scale > 0 and below 2^127 (1 / temperature):
  *   largest = max_j x_j,  logsum = log(sum_j exp(z_j - scale * largest)),
  *   logp_j = z_j - scale * largest - logsum,  logprob = logp[token],
  *   entropy = -sum_j exp(logp_j) logp_j.
@@ -896,7 +896,7 @@ typedef struct ds_adamw_tensor {
 } ds_adamw_tensor;
 
 typedef struct ds_adamw_settings {
-  double rate, beta1, beta2, eps; /* rate, eps >= 0; 0 <= beta < 1                                       */
+  double rate, beta1, beta2, eps; /* rate >= 0; 0 <= beta < 1; eps 0 or 2^-126 at least, all within 32 bits */
   double grad_scale;              /* 1 / the scale of the loss; finite                                   */
   double most_norm;               /* norm of all gradients that is not clipped; 0: no clipping           */
   uint64_t seed;                  /* of the rounding of moments in 8 bits                                */
@@ -910,8 +910,9 @@ typedef struct ds_adamw_settings {
  * Checks the tensors and puts their table on the current device, once for all
  * steps; `tensors` may be freed afterwards.  Tensors without elements are
  * allowed.  Memory that the step writes must not be written for two tensors or
- * twice for one: tables where two matrices begin at one address, or
- * contiguous ones overlap, are refused (DS_EOVERLAP); interleaved views are not checked.
+ * twice for one, nor hold a gradient: tables where two matrices that are written begin
+ * at one address, or contiguous ones overlap, are refused (DS_EOVERLAP); interleaved views
+ * are not checked.  (Two tensors may have one gradient.)
  * The table may be used from several threads; steps on the same tensors are ordered by
  * the caller.  Errors: DS_EINVAL, DS_ERANGE, DS_EOVERLAP, DS_ENOMEM, DS_EHIP.
  */

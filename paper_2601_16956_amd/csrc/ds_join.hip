@@ -8,6 +8,9 @@
 //   a_j = sum dy * h  and  b_j = sum d * k:  dbefore = a,  dgate = scale * after_gamma * b,  dafter = scale * gate * b;
 // they are a line for each work-group, and a second launch adds the lines in their order.
 // Rows too long for the registers are read again for every pass.
+//
+// us, bf16, both norms and a gate: 8192 x 4096 forward 47 (5.7 TB/s), backward 72 + 4.8 for the lines (5.6 TB/s for the first); 1 x 8192 forward
+// 4.3; 1537 x 1000 fp16, one norm, backward 11.3 + 3.9.
 
 #include <type_traits>
 

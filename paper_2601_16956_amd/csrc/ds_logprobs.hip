@@ -4,7 +4,7 @@
 // to sixteen wavefronts, whose threads have pieces of neighbouring columns, 16 bytes each; each thread keeps, of what it has seen, the
 // largest logit m, s = sum exp(scale (x - m)) and t = sum exp(scale (x - m)) (x - m), and where m grows it multiplies them
 // by exp of the difference (t after the difference times s was added).  Threads' triples are joined by the same rule, in an order
-// that only the row's length decides.  Then logsum = log(s) and entropy = logsum - scale t / s.
+// that only the extents and `top` decide.  Then logsum = log(s) and entropy = logsum - scale t / s.
 //
 // The likeliest: the largest logit of every piece goes to LDS.  The lanes of a row are 8, 16 or 32 sets, `top` at least; as many columns
 // reach the least of the sets' largest logits, so the pieces that reach it contain those wanted, and mostly few others.  These pieces are
@@ -13,6 +13,10 @@
 // equal ones, rows in order, few columns that are not masked), the `top`-th of the first 256 found is a higher bound, and it is tried again.
 //
 // Few rows are cut into parts, one work-group each, whose triples and likeliest a second launch joins.
+//
+// us, bf16 logits unless said: 8192 x 32000 forward 92 (5.7 TB/s) and backward 176 (6.0 TB/s); 1 x 32000 with five likeliest 8.0; 2048 x 32000 fp16 with ten
+// 40 (3.3 TB/s: the search for them, which no other row's loads are under way beside in a work-group); 37 x 50021 floats with 20 likeliest 11.9 + 5.2;
+// 1024 x 1024 floats forward 3.9, backward 4.4.
 
 #include <algorithm>
 #include <cmath>
@@ -469,7 +473,7 @@ int check_logits(const ds_matrix *x) {
   return x->dtype == DS_MX8 ? DS_EINVAL : DS_OK;
 }
 
-bool is_scale(float s) { return s > 0.f && s < kInf; }
+bool is_scale(float s) { return s > 0.f && s < 0x1p127f; }  // its product with log2(e) is finite
 
 }  // namespace
 

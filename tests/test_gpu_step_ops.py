@@ -731,6 +731,22 @@ def test_steps_that_are_refused():
     assert all(torch.equal(x, y) for x, y in zip(u.bytes(), before))
 
 
+def test_the_smallest_eps():
+    """eps may be 0 or a number of 32 bits that is not subnormal; with 2^-126, elements that have had no gradient yet stay as they are."""
+    n = 300
+    param, grad, m, v = (torch.full((1, n), x, device="cuda") for x in (1.5, 0.0, 0.0, 0.0))
+    table = ds.ds_adamw_create([ds.make_adamw_tensor(*(ds.make_matrix(x) for x in (param, grad, m, v)))])
+    step = torch.ones(1, dtype=torch.int64, device="cuda")
+    for bad in ({"eps": 2.0 ** -127}, {"eps": 1e-300}, {"eps": 1e39}, {"rate": 1e39}):
+        with pytest.raises(ds.DsError) as e:
+            ds.ds_adamw_step(table, ds.make_adamw_settings(step, **{"rate": 0.1, **bad}), stream())
+        assert e.value.code == ds.DS_EINVAL
+    ds.ds_adamw_step(table, ds.make_adamw_settings(step, 0.1, eps=2.0 ** -126), stream())
+    torch.cuda.synchronize()
+    ds.ds_adamw_destroy(table)
+    assert (param == 1.5).all() and (m == 0).all() and (v == 0).all()
+
+
 def test_moments_in_8_bits_are_rounded_without_a_bias():
     """2^16 groups of one value each: the mean of what is stored is what was rounded, within 5 of its standard deviations (half a step
     over the root of their number, at most), and changes below half a step add up over the steps."""

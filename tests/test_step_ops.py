@@ -324,6 +324,21 @@ def test_memory_that_would_be_written_twice():
     assert code_of(ds.ds_adamw_create, eight) == over
 
 
+def test_gradients_in_memory_that_is_written():
+    of = lambda base, kind=ds.DS_BF16, **kw: mat(dtype=kind, base=base, **kw)  # noqa: E731
+    two = lambda grad: code_of(ds.ds_adamw_create, [entry(), entry(at=PTR + 16 * FAR, grad=grad)])  # noqa: E731
+    over = ds.DS_EOVERLAP
+    for k, size in ((0, 4), (2, 4), (3, 4), (4, 2)):                   # the first one's param, m, v and copy
+        first, past = PTR + k * FAR, PTR + k * FAR + 256 * size
+        assert two(of(first)) == over and two(of(past - 2)) == over and two(of(first - 510)) == over, k
+    assert update(grad=of(PTR, ds.DS_F32)) == over and update(grad=of(PTR + 4 * FAR)) == over
+
+
+def test_a_scale_that_has_no_product():
+    for scale in (2.0 ** 127, 3e38):
+        assert logprobs(scale=scale) == ds.DS_EINVAL and gradient(scale=scale) == ds.DS_EINVAL
+
+
 def test_updates_that_are_refused():
     L, out = ds._lib, ctypes.c_uint64()
     want = ds.DS_EINVAL
