@@ -15,7 +15,7 @@
 // Few rows are cut into parts, one work-group each, whose triples and likeliest a second launch joins.
 //
 // us, bf16 logits unless said: 8192 x 32000 forward 92 (5.7 TB/s) and backward 176 (6.0 TB/s); 1 x 32000 with five likeliest 8.0; 2048 x 32000 fp16 with ten
-// 40 (3.3 TB/s: the search for them, which no other row's loads are under way beside in a work-group); 37 x 50021 floats with 20 likeliest 11.9 + 5.2;
+// 38 (3.5 TB/s: the search for them, beside which none of its work-group's loads are under way); 37 x 50021 floats with 20 likeliest 11.9 + 5.2;
 // 1024 x 1024 floats forward 3.9, backward 4.4.
 
 #include <algorithm>
@@ -216,23 +216,37 @@ __device__ inline void likeliest(const T *row, int count, int64_t begin, uint32_
   uint64_t bound = least == -kInf ? 1 : key_of(least, 0xffffffff);
   int found;
   for (;;) {
-    // pieces that have a column that reaches the bound, or (one of them) might have
+    // pieces that have a column that reaches the bound, or (one of them) might have: four at a time, then two columns of theirs, since each is a
+    // wait for LDS and memory (2048 x 32000 fp16, ten likeliest: 38 us, one by one 40)
 #pragma unroll 1
-    for (int p = threadIdx.x; p < pieces; p += THREADS) {
-      const float peak = peaks[p];
-      if (peak > -kInf && key_of(peak, begin + p * W) >= bound) {
+    for (int p = threadIdx.x; p < pieces; p += 4 * THREADS) {
+      float peak[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) peak[u] = p + u * THREADS < pieces ? peaks[p + u * THREADS] : -kInf;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (!(peak[u] > -kInf && key_of(peak[u], begin + (p + u * THREADS) * W) >= bound)) continue;
         const uint32_t at = atomicAdd(&room.n_hits, 1u);
-        if (at < kCandidates) room.hits[at] = p;
+        if (at < kCandidates) room.hits[at] = p + u * THREADS;
       }
     }
     __syncthreads();
     const int hits = (int)room.n_hits;
 #pragma unroll 1
-    for (int e = threadIdx.x; e < min(hits, kCandidates) * W; e += THREADS) {
-      const int j = (int)room.hits[e / W] * W + e % W;
-      const float x = j < count ? Elem<T>::get(row, j) : -kInf;
-      const uint64_t key = key_of(x, begin + j);
-      if (x > -kInf && key >= bound) {
+    for (int e = threadIdx.x; e < min(hits, kCandidates) * W; e += 2 * THREADS) {
+      float x[2];
+      int j[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int of = min(e + u * THREADS, min(hits, kCandidates) * W - 1);
+        j[u] = (int)room.hits[of / W] * W + of % W;
+        x[u] = Elem<T>::get(row, min(j[u], count - 1));
+        if (j[u] >= count || of != e + u * THREADS) x[u] = -kInf;
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint64_t key = key_of(x[u], begin + j[u]);
+        if (!(x[u] > -kInf && key >= bound)) continue;
         const uint32_t at = atomicAdd(&room.count, 1u);
         if (at < kCandidates) room.keys[at] = key;
       }
