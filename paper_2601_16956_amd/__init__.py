@@ -1085,11 +1085,17 @@ def ds_adamw_squares_workspace(table: int) -> int:
     return out.value
 
 
+_number_types: dict = {}
+
+
 def _one(v, dtype: str, what: str):
     """The address of a number in device memory: an address as it is, or that of a torch tensor of one element."""
     if v is None or not hasattr(v, "data_ptr"):
         return v
-    if str(v.dtype) != "torch." + dtype:
+    if not _number_types:
+        import torch
+        _number_types.update(int64=torch.int64, float32=torch.float32, float64=torch.float64)
+    if v.dtype is not _number_types[dtype]:
         raise TypeError(f"{what} is {v.dtype}, not {dtype}")
     if not v.is_cuda:
         raise ValueError(f"{what} is not in device memory")
