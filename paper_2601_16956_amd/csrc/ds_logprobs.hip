@@ -6,16 +6,17 @@
 // by exp of the difference (t after the difference times s was added).  Threads' triples are joined by the same rule, in an order
 // that only the extents and `top` decide.  Then logsum = log(s) and entropy = logsum - scale t / s.
 //
-// The likeliest: the largest logit of every piece goes to LDS.  The lanes of a row are 8, 16 or 32 sets, `top` at least; as many columns
-// reach the least of the sets' largest logits, so the pieces that reach it contain those wanted, and mostly few others.  These pieces are
-// read again, one by each thread, and what reaches the bound is put into LDS, where each is ranked by counting those in front of it.
+// The likeliest: the largest logit of every piece goes to LDS.  The threads of a row are 64 sets, and the bound is the `top`-th of the sets'
+// largest logits: as many columns reach it, so the pieces that reach it contain those wanted, and mostly few others (of logits in any order, 64 log(64 /
+// (64 - top)) columns: 24 for 20).  These pieces are read again, an element by each thread, and what reaches the bound is put into LDS, where each is
+// ranked by counting those in front of it.
 // Columns are in the order of a key of their logit and place, which no two share.  Where more reach the bound than LDS has room for (many
 // equal ones, rows in order, few columns that are not masked), the `top`-th of the first 256 found is a higher bound, and it is tried again.
 //
 // Few rows are cut into parts, one work-group each, whose triples and likeliest a second launch joins.
 //
-// us, bf16 logits unless said: 8192 x 32000 forward 92 (5.7 TB/s) and backward 176 (6.0 TB/s); 1 x 32000 with five likeliest 8.0; 2048 x 32000 fp16 with ten
-// 38 (3.5 TB/s: the search for them, beside which none of its work-group's loads are under way); 37 x 50021 floats with 20 likeliest 11.9 + 5.2;
+// us, bf16 logits unless said: 8192 x 32000 forward 92 (5.7 TB/s) and backward 176 (6.0 TB/s); 1 x 32000 with five likeliest 7.7; 2048 x 32000 fp16 with ten
+// 32 (4.1 TB/s: the search for them, beside which none of its work-group's loads are under way); 37 x 50021 floats with 20 likeliest 7.6 + 5.2;
 // 1024 x 1024 floats forward 3.9, backward 4.4.
 
 #include <algorithm>
@@ -167,10 +168,12 @@ __device__ inline Triple wave_triple(Triple a, float c) {
 template <int THREADS>
 struct Room {
   Triple triples[THREADS / 64];
-  float sets[64];
+  alignas(16) float sets[64];
+  alignas(16) float least[4];
   uint64_t keys[kCandidates];
   uint64_t bound;
   uint32_t hits[kCandidates];
+  uint16_t threads[THREADS];
   uint32_t n_hits, count;
 };
 
@@ -201,35 +204,56 @@ __device__ inline int rank_of(uint64_t key, const uint64_t *keys, int count) {
 template <typename T, int THREADS, typename Put>
 __device__ inline void likeliest(const T *row, int count, int64_t begin, uint32_t top, float m, const float *peaks, Room<THREADS> &room, Put put) {
   constexpr int W = kColumns<T>;
-  const int pieces = (count + W - 1) / W;
-  // lanes in 64 sets, then sets in 8, 16 or 32
+  const int pieces = (count + W - 1) / W, lane = threadIdx.x & 63;
+  const int shift = pieces <= THREADS ? 0 : min(32 - __clz((pieces - 1) / THREADS), 6);  // lanes of a thread's pieces, as a power of two
+  const float most = m;
+  // threads in 64 sets
   if (THREADS >= 256) m = larger(m, moved<0xB1, 0xf>(m, m)), m = larger(m, moved<0x4E, 0xf>(m, m));
   if (THREADS >= 1024) m = larger(m, moved<0x141, 0xf>(m, m)), m = larger(m, moved<0x140, 0xf>(m, m));
   if (threadIdx.x == 0) room.n_hits = room.count = 0;
   if (threadIdx.x % (THREADS / 64) == 0) room.sets[threadIdx.x / (THREADS / 64)] = m;
   __syncthreads();
-  float set = room.sets[threadIdx.x & 63];
-  set = larger(set, moved<0xB1, 0xf>(set, set));
-  if (top <= 16) set = larger(set, moved<0x4E, 0xf>(set, set));
-  if (top <= 8) set = larger(set, moved<0x141, 0xf>(set, set));
-  const float least = -all_max(-set);
+  // the `top`-th of the 64, of equal ones the first that so many are not larger than: four lanes a set where there are as many
+  float least;
+  if (THREADS == 64) {
+    const float set = room.sets[lane];
+    uint32_t larger_ones = 0;
+#pragma unroll
+    for (int q = 0; q < 64; ++q) larger_ones += room.sets[q] > set;
+    least = -all_max(larger_ones < top ? -set : -kInf);
+  } else {
+    if (threadIdx.x < 256) {
+      const float set = room.sets[threadIdx.x / 4];
+      int larger_ones = 0;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) larger_ones += room.sets[q / 4 * 16 + (threadIdx.x & 3) * 4 + q % 4] > set;
+      larger_ones += __builtin_amdgcn_update_dpp(0, larger_ones, 0xB1, 0xf, 0xf, true);
+      larger_ones += __builtin_amdgcn_update_dpp(0, larger_ones, 0x4E, 0xf, 0xf, true);
+      const float of_wave = all_max(larger_ones < (int)top ? -set : -kInf);
+      if (lane == 0) room.least[threadIdx.x / 64] = of_wave;
+    }
+    __syncthreads();
+    least = -larger(larger(room.least[0], room.least[1]), larger(room.least[2], room.least[3]));
+  }
   uint64_t bound = least == -kInf ? 1 : key_of(least, 0xffffffff);
   int found;
   for (;;) {
-    // pieces that have a column that reaches the bound, or (one of them) might have: four at a time, then two columns of theirs, since each is a
-    // wait for LDS and memory (2048 x 32000 fp16, ten likeliest: 38 us, one by one 40)
+    // Pieces that have a column that reaches the bound, or (one of them) might have: of the threads whose largest logit does, whose pieces the
+    // lanes of their wavefront share.
+    const bool some = most > -kInf && key_of(most, 0) >= bound;
+    const uint64_t mask = __ballot(some);
+    if (some) room.threads[threadIdx.x / 64 * 64 + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = (uint16_t)threadIdx.x;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-    for (int p = threadIdx.x; p < pieces; p += 4 * THREADS) {
-      float peak[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) peak[u] = p + u * THREADS < pieces ? peaks[p + u * THREADS] : -kInf;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (!(peak[u] > -kInf && key_of(peak[u], begin + (p + u * THREADS) * W) >= bound)) continue;
+    for (int t = lane >> shift; t < __popcll(mask); t += 64 >> shift)
+#pragma unroll 1
+      for (int p = room.threads[threadIdx.x / 64 * 64 + t] + (lane & ((1 << shift) - 1)) * THREADS; p < pieces; p += THREADS << shift) {
+        const float peak = peaks[p];
+        if (!(peak > -kInf && key_of(peak, begin + p * W) >= bound)) continue;
         const uint32_t at = atomicAdd(&room.n_hits, 1u);
-        if (at < kCandidates) room.hits[at] = p + u * THREADS;
+        if (at < kCandidates) room.hits[at] = p;
       }
-    }
     __syncthreads();
     const int hits = (int)room.n_hits;
 #pragma unroll 1
@@ -263,13 +287,20 @@ __device__ inline void likeliest(const T *row, int count, int64_t begin, uint32_
     __syncthreads();
     bound = room.bound;
   }
-  if (threadIdx.x < 8 && found + threadIdx.x < kCandidates) room.keys[found + threadIdx.x] = 0;
+  if (threadIdx.x < 32 && found + threadIdx.x < kCandidates) room.keys[found + threadIdx.x] = 0;
   __syncthreads();
+  // four lanes a key, each of which compares it with every fourth eight
 #pragma unroll 1
-  for (int at = threadIdx.x; at < found; at += THREADS) {
+  for (int at = threadIdx.x / 4; at < found; at += THREADS / 4) {
     const uint64_t key = room.keys[at];
-    const int rank = rank_of(key, room.keys, found);
-    if (rank < (int)top) put(rank, key);
+    int rank = 0;
+#pragma unroll 1
+    for (int k = (threadIdx.x & 3) * 8; k < found; k += 32)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) rank += room.keys[k + e] > key;
+    rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, true);
+    rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, true);
+    if ((threadIdx.x & 3) == 0 && rank < (int)top) put(rank, key);
   }
   for (int rank = found + threadIdx.x; rank < (int)top; rank += THREADS) put(rank, 0);
 }
@@ -462,8 +493,8 @@ constexpr int64_t kStream = 64 << 20;
 
 // Parts of a row: where few rows of more than kWhole columns leave most of the card idle, so many that the work-groups are about as many as the
 // CUs, each of at least kLeast columns, and no more candidates than the kernel that joins them has threads; but as many as it takes where the
-// likeliest are looked for.  bf16, us of both kernels, whole / in parts of 32768 columns / of 8192: 1 x 32000 with five likeliest 7.5 / - / 10.0,
-// 1 x 128000 - / 12.4 / 10.9 and without them 9.5 / 7.3 / 6.7, 16 x 128000 with five - / 14.1 / 12.6, 1 x 500000 without 28.8 / 7.8 / 6.8.
+// likeliest are looked for.  bf16, us of both kernels, whole / in parts of 32768 columns / of 8192: 1 x 32000 with five likeliest 7.0 / - / 9.5,
+// 1 x 128000 - / 11.4 / 10.7 and without them 9.5 / 7.3 / 6.7, 16 x 128000 with five - / 13.0 / 12.0, 1 x 500000 without 28.8 / 7.8 / 6.8.
 constexpr int64_t kWhole = 32768, kLeast = 8192;
 int64_t part_cols_of(int64_t cols, int64_t parts) { return ((cols + parts - 1) / parts + 7) / 8 * 8; }
 int64_t parts_of(int64_t rows, int64_t cols, uint32_t top, int64_t size) {
@@ -534,9 +565,11 @@ extern "C" int ds_logprobs(const ds_matrix *logits, float scale, const int64_t *
       const auto rows_with = [&](auto likeliest) -> int {
         constexpr bool TOP = decltype(likeliest)::value;
         // One wavefront a row, four, or sixteen.  bf16, us: 4096 rows of 1024 columns 5.0 / 9.2 / -, of 4096 9.3 / 11.9 / -, of 8192 14.9 / 15.0 /
-        // -; 64 rows of 2048 3.3 / - / 4.0; 200 rows of 32000 - / 6.5 / 6.4, 300 rows - / 8.2 / 10.2, 512 rows with ten likeliest - / 17 / 22.
+        // -; 64 rows of 2048 3.3 / - / 4.0; 200 rows of 32000 - / 6.5 / 6.4, 300 rows - / 8.2 / 10.2.  With five to twenty likeliest: 4096 rows of 2048 9.8 /
+        // 21 / -, of 8192 21.2 / 25.0 / -, of 16000 44 / 38 / -; 3000 rows of 8000 18.1 / 21.5 / -, 1024 rows of 8192 9.2 / 8.8 / -; 512 rows of
+        // 32000 - / 12.2 / 17.4.
         const int64_t bytes = cols * (int64_t)sizeof(T);
-        if (parts == 1 && bytes <= (rows > 256 ? 8192 : 4096)) return launch(ds_logprobs_kernel<T, 64, E, TOP>, 64, rows, pieces);
+        if (parts == 1 && bytes <= (rows > 2048 ? 16384 : rows > 256 ? 8192 : 4096)) return launch(ds_logprobs_kernel<T, 64, E, TOP>, 64, rows, pieces);
         if (rows * parts > 256) return launch(ds_logprobs_kernel<T, 256, E, TOP>, 256, rows * parts, pieces);
         return launch(ds_logprobs_kernel<T, 1024, E, TOP>, 1024, rows * parts, pieces);
       };
