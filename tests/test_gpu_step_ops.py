@@ -395,6 +395,21 @@ def test_logprobs_of_rows_in_order(cols):
             check_probabilities(np.tile(rows, (times, 1)), kind, np.zeros(5 * times, np.int64), 1.0, 32)
 
 
+@pytest.mark.parametrize("kind,cols", [("bf16", 8000), ("f16", 4097), ("f32", 4001)])
+def test_logprobs_of_many_rows(kind, cols):
+    """Rows of one wavefront, whose lanes have several pieces each: in any order, in order, equal, and with hardly a column that is not masked."""
+    rng = np.random.default_rng(cols)
+    x = logits(rng, 2049, cols)
+    x[:100] = np.linspace(5, -5, cols)
+    x[100:200] = np.linspace(-5, 5, cols)
+    x[200:300] = np.round(x[200:300])
+    x[300:400] = 1.0
+    x[400:500, 3:] = -np.inf
+    x[500:600][rng.random((100, cols)) < 0.995] = -np.inf
+    x[600:610] = -np.inf
+    check_probabilities(x, kind, rng.integers(-1, cols + 1, 2049), 1.0, 20, pad=3)
+
+
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("cols", [16, 3000, 40000])
 def test_logprobs_of_special_rows(cols, kind):
