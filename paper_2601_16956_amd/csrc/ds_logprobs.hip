@@ -16,7 +16,7 @@
 // Few rows are cut into parts, one work-group each, whose triples and likeliest a second launch joins.
 //
 // us, bf16 logits unless said: 8192 x 32000 forward 92 (5.7 TB/s) and backward 176 (6.0 TB/s); 1 x 32000 with five likeliest 7.7; 2048 x 32000 fp16 with ten
-// 32 (4.1 TB/s: the search for them, beside which none of its work-group's loads are under way); 37 x 50021 floats with 20 likeliest 7.6 + 5.2;
+// 32 (4.1 TB/s: the search for them, beside which none of its work-group's loads are under way); 37 x 50021 floats with 20 likeliest 7.6 + 4.4;
 // 1024 x 1024 floats forward 3.9, backward 4.4.
 
 #include <algorithm>
@@ -199,6 +199,17 @@ __device__ inline int rank_of(uint64_t key, const uint64_t *keys, int count) {
   return rank;
 }
 
+// The same by four neighbouring lanes, each of which compares every fourth eight.
+__device__ inline int rank_of_four(uint64_t key, const uint64_t *keys, int count) {
+  int rank = 0;
+#pragma unroll 1
+  for (int k = (threadIdx.x & 3) * 8; k < count; k += 32)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rank += keys[k + e] > key;
+  rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, true);
+  return rank + __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, true);
+}
+
 // The likeliest of `count` columns from row[0] on, handed to put(rank, key) by one thread each.  `m`: the thread's largest logit, `peaks`: its
 // pieces' (every THREADS-th); `begin`: the number of the first column.
 template <typename T, int THREADS, typename Put>
@@ -289,17 +300,10 @@ __device__ inline void likeliest(const T *row, int count, int64_t begin, uint32_
   }
   if (threadIdx.x < 32 && found + threadIdx.x < kCandidates) room.keys[found + threadIdx.x] = 0;
   __syncthreads();
-  // four lanes a key, each of which compares it with every fourth eight
 #pragma unroll 1
   for (int at = threadIdx.x / 4; at < found; at += THREADS / 4) {
     const uint64_t key = room.keys[at];
-    int rank = 0;
-#pragma unroll 1
-    for (int k = (threadIdx.x & 3) * 8; k < found; k += 32)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) rank += room.keys[k + e] > key;
-    rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, true);
-    rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, true);
+    const int rank = rank_of_four(key, room.keys, found);
     if ((threadIdx.x & 3) == 0 && rank < (int)top) put(rank, key);
   }
   for (int rank = found + threadIdx.x; rank < (int)top; rank += THREADS) put(rank, 0);
@@ -380,15 +384,17 @@ __global__ __launch_bounds__(THREADS) void ds_logprobs_kernel(Forward a) {
   }
 }
 
-// The parts of a row joined: a work-group has a row.  Its likeliest so far, and as many of the parts' as there are threads left, are ranked
-// until all have been.
+// The parts of a row joined: a work-group has a row, of 64 threads, or 1024 with the likeliest.  Those so far, and as many of the parts' as the 256
+// places have room for, are ranked by four threads each until all have been.  (37 x 6 parts with 20 each: 4.4 us, by one thread each
+// 5.7; 8 parts with 32 each 5.6 and 7.4.)
 constexpr int kMostKeys = 256 - (int)DS_TOP_MOST;
 template <typename T, bool ENTROPY>
-__global__ __launch_bounds__(256) void ds_logprobs_join_kernel(Forward a) {
-  __shared__ uint64_t keys[256], best[DS_TOP_MOST];
+__global__ __launch_bounds__(1024) void ds_logprobs_join_kernel(Forward a) {
+  alignas(16) __shared__ uint64_t keys[256];
+  __shared__ uint64_t best[DS_TOP_MOST];
   const float c = a.scale * kLog2e;
   for (int64_t i = blockIdx.x; i < a.rows; i += gridDim.x) {
-    const int lane = threadIdx.x & 63, spare = threadIdx.x - (int)DS_TOP_MOST;
+    const int lane = threadIdx.x & 63, place = threadIdx.x / 4, quarter = threadIdx.x & 3, spare = place - (int)DS_TOP_MOST;
     const int64_t token = token_of(a, i), count = (int64_t)a.parts * a.top;
     const float at = token >= 0 ? Elem<T>::get(a.x.base, i * a.x.stride + token) : 0.f;
     uint64_t key = spare >= 0 && spare < count ? a.keys[i * count + spare] : 0;
@@ -404,14 +410,16 @@ __global__ __launch_bounds__(256) void ds_logprobs_join_kernel(Forward a) {
     if (!a.top) continue;
     for (int64_t first = 0; first < count; first += kMostKeys) {
       __syncthreads();
-      if (spare < 0) key = first ? best[threadIdx.x] : 0;
+      if (spare < 0) key = first ? best[place] : 0;
       else if (first) key = first + spare < count ? a.keys[i * count + first + spare] : 0;
-      keys[threadIdx.x] = key;
+      if (quarter == 0) keys[place] = key;
       __syncthreads();
-      if (spare < 0) best[threadIdx.x] = 0;
+      if (spare < 0) best[place] = 0;
       __syncthreads();
-      const int rank = key ? rank_of(key, keys, (int)(count - first < kMostKeys ? count - first : kMostKeys) + (int)DS_TOP_MOST) : 256;
-      if (rank < (int)a.top) best[rank] = key;
+      if (key) {
+        const int rank = rank_of_four(key, keys, (int)(count - first < kMostKeys ? count - first : kMostKeys) + (int)DS_TOP_MOST);
+        if (quarter == 0 && rank < (int)a.top) best[rank] = key;
+      }
     }
     __syncthreads();
     if (threadIdx.x < a.top) put_top(a, i, threadIdx.x, best[threadIdx.x], r);
@@ -492,7 +500,7 @@ __global__ __launch_bounds__(256) void ds_logprobs_backward_kernel(Backward a) {
 constexpr int64_t kStream = 64 << 20;
 
 // Parts of a row: where few rows of more than kWhole columns leave most of the card idle, so many that the work-groups are about as many as the
-// CUs, each of at least kLeast columns, and no more candidates than the kernel that joins them has threads; but as many as it takes where the
+// CUs, each of at least kLeast columns, and no more candidates than the kernel that joins them has places; but as many as it takes where the
 // likeliest are looked for.  bf16, us of both kernels, whole / in parts of 32768 columns / of 8192: 1 x 32000 with five likeliest 7.0 / - / 9.5,
 // 1 x 128000 - / 11.4 / 10.7 and without them 9.5 / 7.3 / 6.7, 16 x 128000 with five - / 13.0 / 12.0, 1 x 500000 without 28.8 / 7.8 / 6.8.
 constexpr int64_t kWhole = 32768, kLeast = 8192;
@@ -574,7 +582,7 @@ extern "C" int ds_logprobs(const ds_matrix *logits, float scale, const int64_t *
         return launch(ds_logprobs_kernel<T, 1024, E, TOP>, 1024, rows * parts, pieces);
       };
       DS_TRY(top ? rows_with(std::true_type()) : rows_with(std::false_type()));
-      return parts == 1 ? DS_OK : launch(ds_logprobs_join_kernel<T, E>, 256, rows, 0);
+      return parts == 1 ? DS_OK : launch(ds_logprobs_join_kernel<T, E>, top ? 1024 : 64, rows, 0);
     };
     return entropy ? with(std::true_type()) : with(std::false_type());
   });
