@@ -357,7 +357,7 @@ __global__ __launch_bounds__(WIDE * 64) void ds_join_backward_kernel(JoinBackwar
     for (int c = 0; c < 8; ++c) {
       d.v[c] -= flow * h.v[c];
       db.v[c] += d.v[c] * (kRows == 1 ? k.v[c] : k.v[c] * counts);
-      du.v[c] = after * (d.v[c] * w.v[c] - k.v[c] * along);
+      du.v[c] = after * (d.v[c] * w.v[c] - (a.after ? k.v[c] * along : 0.f));  // (without the norm u, which may be no number, is nothing to du)
       d.v[c] *= joins ? a.v.keep : 1.f;
     }
     if (BOTH || a.du.base) put(a.du, i, du);
@@ -466,9 +466,9 @@ __global__ __launch_bounds__(1024) void ds_join_backward_long_kernel(JoinBackwar
       Eight du = {};
       if (joins && a.du.base) {
         const Eight w = weight_of(a.v, j, n);
-        du = RowsOf<T>::get(a.u, i, j, n);
+        if (a.after) du = RowsOf<T>::get(a.u, i, j, n);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) du.v[k] = r.after * (d.v[k] * w.v[k] - du.v[k] * r.after * along);
+        for (int k = 0; k < 8; ++k) du.v[k] = r.after * (d.v[k] * w.v[k] - du.v[k] * r.after * along);  // (without the norm du and `along` are 0)
         put_up_to8<T>(a.du.base, i * a.du.stride + j, n, du);
       }
       if (a.dx.base) {

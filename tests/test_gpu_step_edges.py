@@ -1,0 +1,44 @@
+"""The operators at a step's joints where their inputs have no numbers, against their definitions in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_16956_amd as ds
+from oracle import training as T
+from test_gpu_step_ops import Joint, back, floats, hidden
+from test_gpu_training_ops import E, TINY, TYPES, U, Mat, within
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- joints --------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("cols", [3, 8, 300, 513, 1000, 2049, 4096, 4100, 8192, 8200, 20003])
+def test_without_the_norm_behind_the_block_its_gradient_does_not_depend_on_it(cols, kind):
+    """du = scale * gate * d: rows of u that are no numbers, as padding may be, are nothing to it."""
+    rng = np.random.default_rng(cols)
+    rows = 6
+    for before in (False, True):
+        j = Joint(rng, cols, kind, False, before, True)
+        u, out, dout, dy = hidden(rng, rows, cols), hidden(rng, rows, cols), rng.standard_normal((rows, cols)), rng.standard_normal((rows, cols))
+        dout[1], dy[1] = 0, 0
+        rb = torch.from_numpy(T.rstd(Mat(out, kind).np(), j.eps).astype(np.float32)).cuda() if before else None
+
+        def run(u, sums, into_u=False):
+            m = [Mat(x, kind) for x in (u, out, dout, dy)]
+            du, dx, room = m[0] if into_u else Mat(np.ones((rows, cols)), kind), Mat(np.ones((rows, cols)), kind), floats(cols)[0]
+            back(j, m[2].m, m[3].m if before else None, m[0].m, m[1].m if before else None, None, rb, du.m, dx.m,
+                 (None, room if sums else None, None), rows, cols)
+            assert du.rest_untouched() and dx.rest_untouched()
+            return du, dx, room
+        clean = run(u, True)
+        lost = u.copy()
+        lost[1, 0], lost[1, cols - 1], lost[4, cols // 2], lost[5] = np.inf, np.nan, -np.inf, np.nan
+        for sums, into_u in ((True, False), (False, False), (True, True)):
+            dirty = run(lost, sums, into_u)
+            assert torch.equal(dirty[0].t, clean[0].t) and torch.equal(dirty[1].t, clean[1].t) and not dirty[0].t[1].any()
+        if not before:
+            want = j.scale * j.g * Mat(dout, kind).np()
+            # the scale as a float, its product with the gate, that with d, and the rounding to the type
+            within(clean[0].np(), want, np.abs(want) * (U[kind] + 3 * E * (1 + U[kind])) + TINY[kind])
