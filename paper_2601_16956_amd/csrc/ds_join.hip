@@ -319,7 +319,8 @@ __global__ __launch_bounds__(WIDE * 64) void ds_join_backward_kernel(JoinBackwar
     const Row now = next;
     if (kAhead) ask(next, first + stride < a.rows ? i + stride : i);
     const float before = a.before ? now.before : 0.f, after = a.after ? now.after : 1.f;
-    const float counts = kRows == 1 || i < a.rows ? 1.f : 0.f;
+    // (chosen by it, not multiplied with it: a row may have infinities; the wavefront's lanes have one row)
+    const bool counts = kRows == 1 || __builtin_amdgcn_readfirstlane((int)(i < a.rows));
     Eight d = RowsOf<T>::value(now.d, 8), k = RowsOf<T>::value(now.u, 8), y = RowsOf<T>::value(now.y, 8), h = RowsOf<T>::value(now.o, 8);
     float sum[3] = {};
 #pragma unroll
@@ -327,7 +328,7 @@ __global__ __launch_bounds__(WIDE * 64) void ds_join_backward_kernel(JoinBackwar
       d.v[c] = a.dout.base ? d.v[c] : 0.f;
       y.v[c] = a.before ? y.v[c] : 0.f, h.v[c] = a.before ? h.v[c] * before : 0.f;
       k.v[c] = joins ? k.v[c] * after : 0.f;
-      da.v[c] += y.v[c] * (kRows == 1 ? h.v[c] : h.v[c] * counts);
+      da.v[c] += counts ? y.v[c] * h.v[c] : 0.f;
       y.v[c] *= g.v[c];
       d.v[c] += before * y.v[c];
       const bool own = WHOLE || c >= others;
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(WIDE * 64) void ds_join_backward_kernel(JoinBackwar
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
       d.v[c] -= flow * h.v[c];
-      db.v[c] += d.v[c] * (kRows == 1 ? k.v[c] : k.v[c] * counts);
+      db.v[c] += counts ? d.v[c] * k.v[c] : 0.f;
       du.v[c] = after * (d.v[c] * w.v[c] - (a.after ? k.v[c] * along : 0.f));  // (without the norm u, which may be no number, is nothing to du)
       d.v[c] *= joins ? a.v.keep : 1.f;
     }

@@ -42,3 +42,30 @@ def test_without_the_norm_behind_the_block_its_gradient_does_not_depend_on_it(co
             want = j.scale * j.g * Mat(dout, kind).np()
             # the scale as a float, its product with the gate, that with d, and the rounding to the type
             within(clean[0].np(), want, np.abs(want) * (U[kind] + 3 * E * (1 + U[kind])) + TINY[kind])
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("cols", [5, 200, 1000, 2000, 4000, 8000, 8200])
+def test_sums_of_a_joint_are_infinite_where_one_of_their_terms_is(cols, kind):
+    """An infinity in the last row, however many rows there are: no other row has a part in it, and none of it in other columns."""
+    rng = np.random.default_rng(cols)
+    j = Joint(rng, cols, kind, False, True, True)
+    for rows in (1, 2, 3, 7, 18):
+        make = lambda: Mat(1 + rng.random((rows, cols)), kind)  # noqa: E731
+        dout, dy, u, out, du, dx = (make() for _ in range(6))
+        u.t[rows - 1, 1], dy.t[rows - 1, cols - 1] = np.inf, -np.inf
+        rb = torch.ones(rows, device="cuda")
+        (dg, dg_rest), (db, db_rest) = floats(cols), floats(cols)
+        back(j, dout.m, dy.m, u.m, out.m, None, rb, du.m, dx.m, (None, None, db), rows, cols)
+        want = (dy.np() * out.np()).sum(0)
+        got = db.double().cpu().numpy()
+        assert want[-1] == got[-1] == -np.inf and np.isfinite(got[:-1]).all()
+        within(got[:-1], want[:-1], np.abs(want[:-1]) * (rows + 4) * E)     # a product and a chain of sums, all of one sign
+        # the gate's, of a joint without norms
+        plain = Joint(np.random.default_rng(cols), cols, kind, False, False, True)
+        back(plain, dout.m, None, u.m, None, None, None, du.m, dx.m, (None, dg, None), rows, cols)
+        want = plain.scale * (dout.np() * u.np()).sum(0)
+        got = dg.double().cpu().numpy()
+        assert want[1] == got[1] == np.inf and np.isfinite(np.delete(got, 1)).all()
+        within(np.delete(got, 1), np.delete(want, 1), np.delete(np.abs(want), 1) * (rows + 8) * E)
+        assert dg_rest() and db_rest()
