@@ -141,6 +141,8 @@ __device__ inline int64_t token_of(const Forward &a, int64_t i) {
   const int64_t token = a.tokens ? a.tokens[i] : -1;
   return token >= 0 && token < a.cols ? token : -1;
 }
+// scale * (x - m).  (A difference of 2^128 or more is no float; its product with a scale below 1 may be.)
+__device__ inline float scaled(const Forward &a, float x, float m) { return a.scale < 1.f ? 2.f * a.scale * (0.5f * x - 0.5f * m) : a.scale * (x - m); }
 // A row's numbers out of its triple.  `at`: the logit of the token, if there is one.
 __device__ inline void put_row(const Forward &a, int64_t i, Triple r, bool given, float at) {
   const bool none = r.m == -kInf && r.s == 0.f;
@@ -149,12 +151,12 @@ __device__ inline void put_row(const Forward &a, int64_t i, Triple r, bool given
   if (a.largest) a.largest[i] = bad ? nan : r.m;
   if (a.logsum) a.logsum[i] = bad ? nan : logsum;
   if (a.entropy) a.entropy[i] = bad ? nan : none ? 0.f : logsum - a.scale * (r.t / r.s);
-  if (a.logprob) a.logprob[i] = !given ? 0.f : bad ? nan : at == -kInf ? -kInf : a.scale * (at - r.m) - logsum;
+  if (a.logprob) a.logprob[i] = !given ? 0.f : bad ? nan : at == -kInf ? -kInf : scaled(a, at, r.m) - logsum;
 }
 __device__ inline void put_top(const Forward &a, int64_t i, int rank, uint64_t key, Triple r) {
   const bool bad = !(r.s < kInf);
   if (a.top_tokens) a.top_tokens[i * a.top + rank] = key && !bad ? key_column(key) : -1;
-  if (a.top_logprobs) a.top_logprobs[i * a.top + rank] = bad ? __uint_as_float(0x7fc00000u) : key ? a.scale * (key_logit(key) - r.m) - logf(r.s) : -kInf;
+  if (a.top_logprobs) a.top_logprobs[i * a.top + rank] = bad ? __uint_as_float(0x7fc00000u) : key ? scaled(a, key_logit(key), r.m) - logf(r.s) : -kInf;
 }
 
 template <bool ENTROPY>

@@ -5,7 +5,7 @@ import torch
 
 import paper_2601_16956_amd as ds
 from oracle import training as T
-from test_gpu_step_ops import Joint, back, floats, hidden
+from test_gpu_step_ops import Joint, back, check_probabilities, floats, hidden, logits
 from test_gpu_training_ops import E, TINY, TYPES, U, Mat, within
 
 pytestmark = pytest.mark.gpu
@@ -69,3 +69,19 @@ def test_sums_of_a_joint_are_infinite_where_one_of_their_terms_is(cols, kind):
         assert want[1] == got[1] == np.inf and np.isfinite(np.delete(got, 1)).all()
         within(np.delete(got, 1), np.delete(want, 1), np.delete(np.abs(want), 1) * (rows + 8) * E)
         assert dg_rest() and db_rest()
+
+
+# ---- log probabilities ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [40, 3000, 70000])
+def test_log_probabilities_over_the_whole_range(cols, kind):
+    """Logits further apart than the largest float, and no further than that under the scale."""
+    rng = np.random.default_rng(cols)
+    most = torch.finfo(TYPES[kind][0]).max
+    x = logits(rng, 4, cols)
+    x[0, 0], x[0, 1:] = most, -most
+    x[1, 5], x[1, 6] = most, most / 2
+    x[2] *= most / 16
+    for scale in (0.5, 0.125, 2.0 ** -40, 1.0):
+        check_probabilities(x, kind, np.array([1, 7, 3, 4]), scale, 8)
