@@ -825,7 +825,7 @@ int ds_join_backward(const ds_join *join, const ds_matrix *dout, const ds_matrix
 
 /*
  * Log probabilities of given tokens.  With z = scale * x over a row of the logits
- * x (DS_F32, DS_BF16, DS_F16; ROWS), scale > 0 and below 2^127 (1 / temperature):
+ * x (DS_F32, DS_BF16, DS_F16; ROWS), scale from 2^-64 to below 2^127 (1 / temperature):
  *   largest = max_j x_j,  logsum = log(sum_j exp(z_j - scale * largest)),
  *   logp_j = z_j - scale * largest - logsum,  logprob = logp[token],
  *   entropy = -sum_j exp(logp_j) logp_j.

@@ -528,7 +528,9 @@ int check_logits(const ds_matrix *x) {
   return x->dtype == DS_MX8 ? DS_EINVAL : DS_OK;
 }
 
-bool is_scale(float s) { return s > 0.f && s < 0x1p127f; }  // its product with log2(e) is finite
+// Its product with log2(e) is finite, and that with a difference of logits which no float holds (2^128 or more: an infinity) would be beyond every
+// exponential's range too; sums of differences times their exponentials, each at most 1 / scale, are floats.
+bool is_scale(float s) { return s >= 0x1p-64f && s < 0x1p127f; }
 
 }  // namespace
 

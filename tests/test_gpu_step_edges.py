@@ -5,7 +5,7 @@ import torch
 
 import paper_2601_16956_amd as ds
 from oracle import training as T
-from test_gpu_step_ops import Joint, back, check_probabilities, floats, hidden, logits
+from test_gpu_step_ops import Joint, back, check_gradient, check_probabilities, floats, hidden, logits
 from test_gpu_training_ops import E, TINY, TYPES, U, Mat, within
 
 pytestmark = pytest.mark.gpu
@@ -85,3 +85,19 @@ def test_log_probabilities_over_the_whole_range(cols, kind):
     x[2] *= most / 16
     for scale in (0.5, 0.125, 2.0 ** -40, 1.0):
         check_probabilities(x, kind, np.array([1, 7, 3, 4]), scale, 8)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [40, 3000, 70000])
+def test_log_probabilities_at_the_least_scale(cols, kind):
+    """2^-64: logits of 2^64 under it, the whole range of the type, and rows in which sums of differences are as large as they can be."""
+    rng = np.random.default_rng(cols)
+    most = torch.finfo(TYPES[kind][0]).max
+    x = logits(rng, 6, cols) * 2.0 ** 64
+    x[1, 0], x[1, 1:] = most, -most
+    x[2, ::2], x[2, 1::2] = 0.0, -2.0 ** 64               # one in e of the likeliest: the largest product with its difference
+    x[3, 5:] = -np.inf
+    x[4, ::3] = -most
+    tokens = np.array([1, 0, 3, 4, 2, 7])
+    check_probabilities(x, kind, tokens, 2.0 ** -64, 8)
+    check_gradient(x, kind, tokens, 2.0 ** -64, rng.standard_normal(6), rng.standard_normal(6))

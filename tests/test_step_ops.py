@@ -358,3 +358,10 @@ def test_checkpoints_of_values_from_0_on_that_are_none():
     assert code_of(ds.ds_layernorm_forward, x, PTR, PTR, ds.DS_BF16, 1e-5, mat(), PTR, PTR, eight) == want
     assert code_of(ds.ds_matmul, mat(4, 64, dtype=ds.DS_UF8), mat(64, 8), mat(4, 8), None, PTR, 1 << 40) == want
     assert code_of(ds.ds_activation_backward, x, eight, ds.DS_ACT_GELU, mat(), None) == want
+
+
+def test_a_scale_under_which_differences_that_no_float_holds_would_count():
+    """3e38 and -3e38 are 6 apart under 1e-38, and infinitely far as floats: refused below 2^-64, where no row can show it."""
+    for scale in (1e-38, 2.0 ** -140, math.nextafter(2.0 ** -64, 0.0) * (1 - 2.0 ** -24)):
+        assert logprobs(scale=scale) == ds.DS_EINVAL and gradient(scale=scale) == ds.DS_EINVAL
+    assert logprobs(x=mat(0, 64, base=None), scale=2.0 ** -64) == ds.DS_OK
