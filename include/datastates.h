@@ -909,7 +909,7 @@ typedef struct ds_adamw_settings {
 /*
  * Checks the tensors and puts their table on the current device, once for all
  * steps; `tensors` may be freed afterwards.  Tensors without elements are
- * allowed.  Memory that the step writes must not be written for two tensors or
+ * allowed; all together have at most 2^37.  Memory that the step writes must not be written for two tensors or
  * twice for one, nor hold a gradient: tables where two matrices that are written begin
  * at one address, or contiguous ones overlap, are refused (DS_EOVERLAP); interleaved views
  * are not checked.  (Two tensors may have one gradient.)

@@ -37,6 +37,7 @@ constexpr int64_t kQuads = kThreads * kEach;   // of a chunk
 // So / by ordinary accesses, us of the step, tables in rotation: float moments 1 M 6.8 / 8.2, 3 M 17.3 / 15.2, 6 M 31 / 29, 17 M 83 / 90, 55 M
 // 242 / 269; moments in 8 bits 6 M 24.2 / 23.8, 25 M 74 / 82, 136 M 362 / 390.
 constexpr int64_t kStream = 8 << 20;
+constexpr int64_t kMostElements = 1ll << 37;   // of a table: more than any device holds with two moments; sizes that are a mistake fill no memory with chunks
 constexpr int64_t kSquareGroups = 2048;        // work-groups of the sum of squares, for each kind of tensors
 constexpr int kSquareChunks = 4;               // chunks that they have on their way at a time
 
@@ -556,6 +557,7 @@ int make_table(const ds_adamw_tensor *from, size_t n, ds_adamw &table) {
     DS_TRY(check_tensor(f, copied));
     const int64_t rows = f.param.rows, cols = f.param.cols;
     if (rows == 0 || cols == 0) continue;
+    if (rows * cols > kMostElements - table.elements) return DS_ERANGE;
     table.elements += rows * cols;
     const bool eight = f.m.dtype == DS_MX8;
     const ds_matrix *all[] = {&f.param, &f.grad, &f.m, &f.v, copied ? &f.copy : nullptr};

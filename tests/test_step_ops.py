@@ -365,3 +365,13 @@ def test_a_scale_under_which_differences_that_no_float_holds_would_count():
     for scale in (1e-38, 2.0 ** -140, math.nextafter(2.0 ** -64, 0.0) * (1 - 2.0 ** -24)):
         assert logprobs(scale=scale) == ds.DS_EINVAL and gradient(scale=scale) == ds.DS_EINVAL
     assert logprobs(x=mat(0, 64, base=None), scale=2.0 ** -64) == ds.DS_OK
+
+
+def test_tables_that_no_device_holds():
+    """Sizes that are a mistake are refused before a record is made for every 2048 elements of them."""
+    large = lambda rows, cols, at, **kw: entry(  # noqa: E731
+        *(mat(rows, cols, dtype=kind, base=at + k * (1 << 50), **kw) for k, kind in enumerate((ds.DS_BF16, ds.DS_BF16, ds.DS_MX8, ds.DS_UF8))), copy=None)
+    most = (1 << 31) - 1
+    assert code_of(ds.ds_adamw_create, [large(most, most, PTR)]) == ds.DS_ERANGE
+    assert code_of(ds.ds_adamw_create, [large(most, 65, PTR)]) == ds.DS_ERANGE
+    assert code_of(ds.ds_adamw_create, [large(1 << 21, 1 << 15, PTR), large(1 << 21, 1 << 15, PTR + (1 << 53)), entry()]) == ds.DS_ERANGE
