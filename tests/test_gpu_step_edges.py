@@ -101,3 +101,22 @@ def test_log_probabilities_at_the_least_scale(cols, kind):
     tokens = np.array([1, 0, 3, 4, 2, 7])
     check_probabilities(x, kind, tokens, 2.0 ** -64, 8)
     check_gradient(x, kind, tokens, 2.0 ** -64, rng.standard_normal(6), rng.standard_normal(6))
+
+
+# ---- joints beyond the range of squares --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cols", [100, 5000, 20003])
+def test_joints_of_squares_beyond_32_bits(cols):
+    """Their sum is infinite, and the norm's factor 0: nothing of the block, a norm of nothing, and other rows as they are."""
+    rng = np.random.default_rng(cols)
+    j = Joint(rng, cols, "f32", True, True, True)
+    u, x = hidden(rng, 3, cols), hidden(rng, 3, cols)
+    u[1] *= 1e25
+
+    def run(u):
+        m = [Mat(a, "f32") for a in (u, x, x, x)]
+        ra, rb = floats(3)[0], floats(3)[0]
+        ds.ds_join_forward(j.m, *[a.m for a in m], ra, rb, torch.cuda.current_stream().cuda_stream)
+        return m[2].t, m[3].t, ra, rb
+    got, want = run(u), run(np.where(np.arange(3)[:, None] == 1, 0.0, u))
+    assert float(got[2][1]) == 0 and all(torch.equal(a, b) for k, (a, b) in enumerate(zip(got, want)) if k != 2)
