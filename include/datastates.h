@@ -776,7 +776,8 @@ int ds_activation_backward(const ds_matrix *dy, const ds_matrix *z, uint32_t act
  *   y   = out * rstd_before * before_gamma  (DS_JOIN_BEFORE),
  *         rstd_before = 1 / sqrt(sum_j out_j^2 / cols + eps)
  * where out counts as it is stored, rounded to its type: the gradient has
- * nothing else to start from.
+ * nothing else to start from.  (Squares and their sums are 32-bit floats: beyond
+ * their range rstd is 0.)
  */
 #define DS_JOIN_AFTER 1u
 #define DS_JOIN_BEFORE 2u
@@ -867,7 +868,7 @@ int ds_logprobs_backward(const ds_matrix *logits, float scale, const int64_t *to
 /*
  * The update, which the gate of the snapshot in flight stands in front of: AdamW
  * over all tensors of a table at once.  With t the number of this step (from 1
- * on), q = sqrt(squares) * grad_scale, and
+ * on), q = sqrt(squares) * |grad_scale|, and
  *   c = grad_scale * (q > most_norm > 0 ? most_norm / q : 1):
  *   g = c * grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   r = settings' rate * tensor's rate,
@@ -875,8 +876,8 @@ int ds_logprobs_backward(const ds_matrix *logits, float scale, const int64_t *to
  * and copy = param, rounded to copy's type (from 32 bits, as param is to its own).
  *
  * Moments are both DS_F32, or m DS_MX8 and v DS_UF8.  The latter are rounded at
- * random, without a bias, where DS_MX8 and DS_UF8 otherwise say to nearest (which would
- * lose every change that is smaller than half a step): with the 16 low bits a
+ * random, without a bias (but for what the codes' limits cut: an m above 127 steps, a v below code 1), where
+ * DS_MX8 and DS_UF8 otherwise say to nearest (which would lose every change that is smaller than half a step): with the 16 low bits a
  * and the 16 high bits b of the element's random number, the code of m is
  * floor(m / step + (a + 1/2) / 2^16), the sum rounded to 32 bits and the code limited
  * to +-127, and that of v is ((bits(v) + 16 b + 8) >> 20) - 8 s.  The random number of
