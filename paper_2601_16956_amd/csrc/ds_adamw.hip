@@ -16,7 +16,8 @@
 //
 // us, of the step and of the sum of squares: 2.4 M elements in 29 tensors, float moments, bf16 gradients and copies (28 bytes in the step) 11 and
 // 5.3; 54.7 M such in one tensor 255 (6.0 TB/s) and 23; 135.8 M with moments in 8 bits (16.1 bytes) 357 (6.1 TB/s) and 52; 2000 tensors of 1 to
-// 65536 elements, 11 M in all, float gradients and moments in 8 bits 38.
+// 65536 elements, 11 M in all, float gradients and moments in 8 bits 38.  54.7 M in one tensor whose rows of 4096 lie apart, float moments 287 (5.3 TB/s) and 45, in
+// 8 bits 163 (5.4 TB/s) and 41.
 
 #include <algorithm>
 #include <cfloat>
@@ -34,8 +35,10 @@ constexpr int kThreads = 256;
 constexpr int kEach = 2;                       // quads of a thread
 constexpr int64_t kQuads = kThreads * kEach;   // of a chunk
 // Elements of a table from which on accesses are not temporal: its state is not to stay in the caches, and nothing else that does is to leave.
-// So / by ordinary accesses, us of the step, tables in rotation: float moments 1 M 6.8 / 8.2, 3 M 17.3 / 15.2, 6 M 31 / 29, 17 M 83 / 90, 55 M
-// 242 / 269; moments in 8 bits 6 M 24.2 / 23.8, 25 M 74 / 82, 136 M 362 / 390.
+// A smaller one's may still be there when the next step comes.  Not temporal / ordinary, us of the step alone, with three tables in turn, then with twelve, whose
+// states no cache holds: float moments 1 M 6.2 / 6.7, 6.4 / 6.9; 3 M 16.2 / 13.6, 16.6 / 19.9; 6 M 30 / 28, 31 / 36; 8 M 40 / 44, 40 / 46; 17 M 83 / 91; 55 M
+// 269 / 294; moments in 8 bits 1 M 6.1 / 6.4, 6.4 / 7.0; 6 M 21.5 / 19.5, 21.4 / 24.7; 12 M 36.5 / 38.0; 25 M 69 / 77; 136 M 360 / 404.  (1 M elements are
+// mostly latency, and either way within half a microsecond.)
 constexpr int64_t kStream = 8 << 20;
 constexpr int64_t kMostElements = 1ll << 37;   // of a table: more than any device holds with two moments; sizes that are a mistake fill no memory with chunks
 constexpr int64_t kSquareGroups = 2048;        // work-groups of the sum of squares, for each kind of tensors

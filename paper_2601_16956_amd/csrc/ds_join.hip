@@ -9,8 +9,9 @@
 // they are a line for each work-group, and a second launch adds the lines in their order.
 // Rows too long for the registers are read again for every pass.
 //
-// us, bf16, both norms and a gate: 8192 x 4096 forward 47 (5.7 TB/s), backward 72 + 4.8 for the lines (5.6 TB/s for the first); 1 x 8192 forward
-// 4.3; 1537 x 1000 fp16, one norm, backward 11.3 + 3.9.
+// us, bf16, both norms and a gate: 8192 x 4096 forward 47 (5.7 TB/s), backward 73 + 4.7 for the lines (5.5 TB/s for the first); 1 x 8192 forward
+// 4.3; 1537 x 1000 fp16, one norm, backward 11.5 + 3.9.  Floats, 8192 x 2048: forward 52 (5.2 TB/s), backward 82 + 4.7 (4.9 TB/s: no row is on its
+// way during another, whose 32-bit words fill the registers).
 
 #include <type_traits>
 
@@ -23,8 +24,7 @@ __device__ inline int columns_left(int64_t cols, int64_t j) {
   return (int)(left < 0 ? 0 : left < 8 ? left : 8);
 }
 
-// The sum of `x` over the `WAVES` wavefronts of a row, in every thread.  `room`: one float per wavefront, another one in every turn: it is
-// written again only behind the barrier of a sum in between.
+// Of rows of any length: the sum of `x` over the work-group's wavefronts, in every thread, by `room` as total_of_row does.
 template <int WAVES>
 __device__ inline float row_sum(float x, float *room) {
   x = wave_sum(x);
@@ -547,7 +547,9 @@ __global__ __launch_bounds__(256) void ds_join_sums_kernel(const float *partial,
   }
 }
 
-// Rows of so many columns fit the registers of a work-group.
+// Rows of so many columns fit the registers of a work-group: two matrices of them forward, four backward.  us, bf16, on either side of it: forward 2048 x 16384
+// 52 (5.1 TB/s), 2048 x 20000, whose second and third passes read again, 101 (3.2); backward 4096 x 8192 74 + 7 (5.0), 2048 x 16384, in three launches
+// that read a matrix two or three times, 43 + 43 + 113 + 5 (2.0).
 constexpr int64_t kLongest = 16384, kLongestBackward = 8192;
 
 int64_t join_groups(int64_t rows, int64_t at_a_time, int64_t most) {
