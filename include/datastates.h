@@ -859,6 +859,7 @@ int ds_logprobs(const ds_matrix *logits, float scale, const int64_t *tokens, flo
  * is needed where it is given.  dlogits: type and extents of logits, ROWS; it may
  * be logits itself.  Rows whose token is none (or dlogprob 0) and whose dentropy is 0, and rows
  * that are masked whole, have zeros whatever is in them; masked columns have p = 0.
+ * (So it is that of whole rows: a part of a cut row which does not have the token would have zeros.)
  * Errors: DS_EINVAL, DS_ERANGE, DS_EHIP.
  */
 int ds_logprobs_backward(const ds_matrix *logits, float scale, const int64_t *tokens, const float *largest,
